@@ -97,6 +97,22 @@ def load() -> ctypes.CDLL:
     lib.mxfp8_mfma_layout_probe.argtypes = [vp, vp, vp, vp, ctypes.c_int32, ctypes.c_int32, vp, vp]
     lib.mxfp8_mfma_layout_probe.restype = ci
     lib.mxfp8_copy_rate_probe.argtypes = [vp, vp, i64, ctypes.c_int32, ctypes.c_int32, vp]
+    lib.mxfp8_expert_rows.argtypes = [i64, ctypes.c_int32, ctypes.c_int32]
+    lib.mxfp8_expert_rows.restype = i64
+    lib.mxfp8_expert_sort_workspace.argtypes = [i64, ctypes.c_int32]
+    lib.mxfp8_expert_sort_workspace.restype = i64
+    lib.mxfp8_expert_sort.argtypes = [vp, ci, i64, ctypes.c_int32, ctypes.c_int32, i64, vp, vp, vp, vp, vp]
+    lib.mxfp8_expert_sort.restype = ci
+    lib.mxfp8_expert_quantize_ex.argtypes = [vp, ci, i64, i64, i64, vp, ctypes.c_int32, vp, vp, ctypes.c_int32, i64, ci, vp, vp, vp, vp, ci, vp]
+    lib.mxfp8_expert_quantize_ex.restype = ci
+    lib.mxfp8_expert_combine.argtypes = [vp, ci, i64, i64, i64, vp, vp, i64, ctypes.c_int32, vp, ci, i64, vp]
+    lib.mxfp8_expert_combine.restype = ci
+    lib.mxfp8_expert_weight_grad.argtypes = [vp, ci, i64, vp, ci, i64, i64, i64, vp, i64, ctypes.c_int32, vp, vp]
+    lib.mxfp8_expert_weight_grad.restype = ci
+    lib.mxfp8_fp4_gemv_ex.argtypes = [vp, i64, vp, vp, i64, i64, i64, vp, ci, i64, ci, vp]
+    lib.mxfp8_fp4_gemv_ex.restype = ci
+    lib.mxfp8_fp4_gemv_grouped_ex.argtypes = [vp, i64, i64, vp, ctypes.c_int32, vp, vp, vp, ctypes.c_int32, i64, i64, i64, vp, ci, i64, ci, vp]
+    lib.mxfp8_fp4_gemv_grouped_ex.restype = ci
     lib.mxfp8_status_string.restype = ctypes.c_char_p
     lib.mxfp8_status_string.argtypes = [ci]
     _lib = lib

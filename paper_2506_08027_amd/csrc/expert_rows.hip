@@ -1,0 +1,238 @@
+// Rows on their way to the experts and back (include/mxfp8_experts.h): the quantizer of sorted rows, the weighted sum of a
+// token's rows, and the gradient of its weights. All three are bound by HBM: no row is stored between them and the products.
+#include "expert_launches.h"
+#include "quantize_tile.h"
+
+namespace mxfp8 {
+
+// ---- quantizer of sorted rows: the tile conversion of quantize_tile.h on rows fetched through the plan ------------------------
+// The rows of a tile, by their token (-1: zeros) and weight, in LDS. BF16 rows times an FP32 weight take the FP32 register layout.
+template <bool SRC_BF16, bool WEIGHTED> struct ExpertRows {
+    static constexpr bool kGiven = true;
+    const uint8_t *src;
+    int64_t ld_bytes;
+    const int32_t *token;
+    const float *weight;
+    __device__ __forceinline__ uint4 load(int r, int64_t c) const
+    {
+        const int t = token[r];
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (t < 0)
+            return v;
+        const uint8_t *p = src + t * ld_bytes + c * (SRC_BF16 ? 2 : 4);
+        if constexpr (!WEIGHTED) {
+            v = *reinterpret_cast<const uint4 *>(p);
+        } else {
+            const float w = weight[r];
+            if constexpr (SRC_BF16) {
+                const uint2 h = *reinterpret_cast<const uint2 *>(p);
+                v = make_uint4(h.x << 16, h.x & 0xFFFF0000u, h.y << 16, h.y & 0xFFFF0000u);
+            } else {
+                v = *reinterpret_cast<const uint4 *>(p);
+            }
+            v = make_uint4(__float_as_uint(w * __uint_as_float(v.x)), __float_as_uint(w * __uint_as_float(v.y)),
+                           __float_as_uint(w * __uint_as_float(v.z)), __float_as_uint(w * __uint_as_float(v.w)));
+        }
+        return v;
+    }
+};
+
+template <bool SRC_BF16, bool WEIGHTED, bool ROW, bool COL, bool TILED>
+__global__ __launch_bounds__(kQuantThreads) void expert_quantize_kernel(
+    const uint8_t *__restrict__ src, int64_t ld_bytes, const int32_t *__restrict__ sources, uint32_t entries, uint32_t slots,
+    const float *__restrict__ weights, const int32_t *__restrict__ group_ends, int groups, int64_t rows, int64_t cols,
+    uint8_t *__restrict__ q_row, uint8_t *__restrict__ s_row, uint8_t *__restrict__ q_colT, uint8_t *__restrict__ s_colT, uint32_t tiles_x)
+{
+    constexpr bool BF16 = SRC_BF16 && !WEIGHTED;  // register layout
+    __shared__ __attribute__((aligned(16))) uint8_t lds_q[COL ? kTile * kTile : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t lds_rs[ROW ? kTile * 4 : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t lds_cs[COL ? kTile * 4 : 16];
+    __shared__ int32_t token[kTile];
+    __shared__ float weight[WEIGHTED ? kTile : 1];
+    const QuantLds lds{lds_q, lds_rs, lds_cs, nullptr, nullptr};
+    const ExpertRows<SRC_BF16, WEIGHTED> rows_of_tile{src, ld_bytes, token, weight};
+    const int tid = threadIdx.x;
+    // tiles of rows that hold a row of an expert
+    const int64_t end = groups ? min(max((int64_t)group_ends[groups - 1], (int64_t)0), rows) : rows;
+    const uint32_t tiles_y = (uint32_t)((end + kTile - 1) / kTile), ntiles = tiles_x * tiles_y;
+    const bool walk_down = COL && cols > end;  // as in quantize.hip
+    for (uint32_t tile = blockIdx.x; tile < ntiles; tile += gridDim.x) {
+        const uint32_t tile_y = walk_down ? tile % tiles_y : tile / tiles_x, tile_x = walk_down ? tile / tiles_y : tile % tiles_x;
+        if (tid < kTile) {
+            const int64_t r = (int64_t)tile_y * kTile + tid;
+            const uint32_t i = r < rows ? (uint32_t)sources[r] : ~0u;
+            token[tid] = i < entries ? (int32_t)(i / slots) : -1;
+            if constexpr (WEIGHTED)
+                weight[tid] = i < entries ? weights[i] : 0.0f;
+        }
+        __syncthreads();
+        quantize_tile<BF16, ROW, COL, TILED, 0, false>(nullptr, rows, cols, 0, q_row, s_row, q_colT, s_colT, nullptr, tile_y, tile_x, tid, lds,
+                                                       &rows_of_tile);
+        __syncthreads();  // the next tile reuses the arrays
+    }
+}
+
+template <bool SRC_BF16, bool WEIGHTED, bool TILED>
+static hipError_t launch_expert_quantize_t(const void *src, int64_t tokens, int64_t cols, int64_t ld, const int32_t *sources, int slots,
+                                           const float *weights, const int32_t *group_ends, int groups, int64_t rows, int axis, uint8_t *q_row,
+                                           uint8_t *s_row, uint8_t *q_colT, uint8_t *s_colT, hipStream_t stream)
+{
+    const int64_t tiles_x = (cols + kTile - 1) / kTile, tiles = tiles_x * ((rows + kTile - 1) / kTile);
+    if (tiles > 0x7FFFFFFF)
+        return hipErrorInvalidConfiguration;
+    int dev = 0, cus = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess)
+        e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+    if (e != hipSuccess)
+        return e;
+    // The host knows the tiles of all rows, not how many of them belong to an expert: a resident grid walks over those that do.
+    const unsigned workgroups = (unsigned)min(tiles, (int64_t)max(cus, 1) * 4);
+    auto kern = axis == 1   ? expert_quantize_kernel<SRC_BF16, WEIGHTED, true, false, TILED>
+                : axis == 2 ? expert_quantize_kernel<SRC_BF16, WEIGHTED, false, true, TILED>
+                            : expert_quantize_kernel<SRC_BF16, WEIGHTED, true, true, TILED>;
+    hipLaunchKernelGGL(kern, dim3(workgroups), dim3(kQuantThreads), 0, stream, static_cast<const uint8_t *>(src), ld * (SRC_BF16 ? 2 : 4), sources,
+                       (uint32_t)(tokens * slots), (uint32_t)slots, weights, group_ends, groups, rows, cols, q_row, s_row, q_colT, s_colT,
+                       (uint32_t)tiles_x);
+    return hipGetLastError();
+}
+
+hipError_t launch_expert_quantize(const void *src, bool bf16, int64_t tokens, int64_t cols, int64_t ld, const int32_t *sources, int slots,
+                                  const float *weights, const int32_t *group_ends, int groups, int64_t rows, int axis, uint8_t *q_row,
+                                  uint8_t *s_row, uint8_t *q_colT, uint8_t *s_colT, bool tiled_scales, hipStream_t stream)
+{
+    auto launch = bf16 ? (weights ? (tiled_scales ? launch_expert_quantize_t<true, true, true> : launch_expert_quantize_t<true, true, false>)
+                                  : (tiled_scales ? launch_expert_quantize_t<true, false, true> : launch_expert_quantize_t<true, false, false>))
+                       : (weights ? (tiled_scales ? launch_expert_quantize_t<false, true, true> : launch_expert_quantize_t<false, true, false>)
+                                  : (tiled_scales ? launch_expert_quantize_t<false, false, true> : launch_expert_quantize_t<false, false, false>));
+    return launch(src, tokens, cols, ld, sources, slots, weights, group_ends, groups, rows, axis, q_row, s_row, q_colT, s_colT, stream);
+}
+
+// ---- sums over a token's rows --------------------------------------------------------------------------------------------------
+// Eight consecutive values as FP32.
+struct Values8 {
+    float v[8];
+};
+template <bool BF16> __device__ __forceinline__ Values8 load8(const uint8_t *p)
+{
+    Values8 r;
+    const uint4 a = *reinterpret_cast<const uint4 *>(p);
+    if constexpr (BF16) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t w = word_at(a, k);
+            r.v[2 * k] = __uint_as_float(w << 16);
+            r.v[2 * k + 1] = __uint_as_float(w & 0xFFFF0000u);
+        }
+    } else {
+        const uint4 b = *reinterpret_cast<const uint4 *>(p + 16);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            r.v[k] = __uint_as_float(word_at(a, k));
+            r.v[4 + k] = __uint_as_float(word_at(b, k));
+        }
+    }
+    return r;
+}
+template <bool BF16> __device__ __forceinline__ void store8(uint8_t *p, const Values8 &x)
+{
+    if constexpr (BF16) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const v2bf h = {(__bf16)x.v[2 * k], (__bf16)x.v[2 * k + 1]};
+            w[k] = __builtin_bit_cast(uint32_t, h);
+        }
+        stream_store(reinterpret_cast<uint4 *>(p), make_uint4(w[0], w[1], w[2], w[3]));
+    } else {
+        stream_store(reinterpret_cast<uint4 *>(p), make_uint4(__float_as_uint(x.v[0]), __float_as_uint(x.v[1]), __float_as_uint(x.v[2]), __float_as_uint(x.v[3])));
+        stream_store(reinterpret_cast<uint4 *>(p + 16), make_uint4(__float_as_uint(x.v[4]), __float_as_uint(x.v[5]), __float_as_uint(x.v[6]), __float_as_uint(x.v[7])));
+    }
+}
+
+constexpr int kRowThreads = 256, kRowWaves = kRowThreads / 64;
+constexpr int kPiece = 512;  // columns of a wavefront: eight a lane
+
+// A wavefront sums kPiece columns of one token; its rows and weights are the same for all lanes.
+template <bool C_BF16, bool OUT_BF16>
+__global__ __launch_bounds__(kRowThreads) void expert_combine_kernel(const uint8_t *__restrict__ c, int64_t rows, int cols, int64_t ld_bytes,
+                                                                     const int32_t *__restrict__ positions, const float *__restrict__ weights,
+                                                                     uint32_t tokens, int slots, uint8_t *__restrict__ out, int64_t ld_out_bytes,
+                                                                     uint32_t pieces)
+{
+    const int lane = threadIdx.x & 63;
+    const uint32_t id = blockIdx.x * kRowWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t token = id / pieces;
+    const int64_t col = (int64_t)(id - token * pieces) * kPiece + lane * 8;
+    if (token >= tokens || col >= cols)
+        return;
+    Values8 sum = {};
+    for (int j = 0; j < slots; ++j) {
+        const int64_t i = (int64_t)token * slots + j;
+        const int32_t r = positions[i];
+        if (r < 0 || r >= rows)
+            continue;
+        const float w = weights ? weights[i] : 1.0f;
+        const Values8 x = load8<C_BF16>(c + r * ld_bytes + col * (C_BF16 ? 2 : 4));
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            sum.v[k] = fmaf(w, x.v[k], sum.v[k]);
+    }
+    store8<OUT_BF16>(out + token * ld_out_bytes + col * (OUT_BF16 ? 2 : 4), sum);
+}
+
+hipError_t launch_expert_combine(const void *c, bool c_bf16, int64_t rows, int64_t cols, int64_t ldc, const int32_t *positions,
+                                 const float *weights, int64_t tokens, int slots, void *out, bool out_bf16, int64_t ld_out, hipStream_t stream)
+{
+    const int64_t pieces = (cols + kPiece - 1) / kPiece, workgroups = (tokens * pieces + kRowWaves - 1) / kRowWaves;
+    if (tokens * pieces > 0x7FFFFFFF)
+        return hipErrorInvalidConfiguration;
+    auto kern = c_bf16 ? (out_bf16 ? expert_combine_kernel<true, true> : expert_combine_kernel<true, false>)
+                       : (out_bf16 ? expert_combine_kernel<false, true> : expert_combine_kernel<false, false>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)workgroups), dim3(kRowThreads), 0, stream, static_cast<const uint8_t *>(c), rows, (int)cols,
+                       ldc * (c_bf16 ? 2 : 4), positions, weights, (uint32_t)tokens, slots, static_cast<uint8_t *>(out), ld_out * (out_bf16 ? 2 : 4),
+                       (uint32_t)pieces);
+    return hipGetLastError();
+}
+
+// ---- gradient of the weights ------------------------------------------------------------------------------------------------------
+// A wavefront takes the dot product of one entry.
+template <bool DY_BF16, bool C_BF16>
+__global__ __launch_bounds__(kRowThreads) void expert_weight_grad_kernel(const uint8_t *__restrict__ dy, int64_t ld_dy_bytes, const uint8_t *__restrict__ c,
+                                                                         int64_t rows, int cols, int64_t ld_bytes,
+                                                                         const int32_t *__restrict__ positions, uint32_t entries, uint32_t slots,
+                                                                         float *__restrict__ dw)
+{
+    const int lane = threadIdx.x & 63;
+    const uint32_t i = blockIdx.x * kRowWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (i >= entries)
+        return;
+    const int32_t r = positions[i];
+    float sum = 0.0f;
+    if (r >= 0 && r < rows) {
+        const uint8_t *a = dy + (int64_t)(i / slots) * ld_dy_bytes, *b = c + r * ld_bytes;
+        for (int64_t col = lane * 8; col < cols; col += kPiece) {
+            const Values8 x = load8<DY_BF16>(a + col * (DY_BF16 ? 2 : 4)), y = load8<C_BF16>(b + col * (C_BF16 ? 2 : 4));
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                sum = fmaf(x.v[k], y.v[k], sum);
+        }
+    }
+    for (int d = 32; d >= 1; d /= 2)
+        sum += __uint_as_float((uint32_t)__shfl_xor((int)__float_as_uint(sum), d, 64));
+    if (lane == 0)
+        dw[i] = sum;
+}
+
+hipError_t launch_expert_weight_grad(const void *dy, bool dy_bf16, int64_t ld_dy, const void *c, bool c_bf16, int64_t rows, int64_t cols,
+                                     int64_t ldc, const int32_t *positions, int64_t tokens, int slots, float *dw, hipStream_t stream)
+{
+    const int64_t entries = tokens * slots, workgroups = (entries + kRowWaves - 1) / kRowWaves;
+    auto kern = dy_bf16 ? (c_bf16 ? expert_weight_grad_kernel<true, true> : expert_weight_grad_kernel<true, false>)
+                        : (c_bf16 ? expert_weight_grad_kernel<false, true> : expert_weight_grad_kernel<false, false>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)workgroups), dim3(kRowThreads), 0, stream, static_cast<const uint8_t *>(dy), ld_dy * (dy_bf16 ? 2 : 4),
+                       static_cast<const uint8_t *>(c), rows, (int)cols, ldc * (c_bf16 ? 2 : 4), positions, (uint32_t)entries, (uint32_t)slots, dw);
+    return hipGetLastError();
+}
+
+}  // namespace mxfp8

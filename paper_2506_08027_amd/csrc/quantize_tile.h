@@ -142,17 +142,23 @@ struct QuantLds {
     uint32_t *src_s;
 };
 
+struct NoRows {
+    static constexpr bool kGiven = false;
+};
+
 // MXSRC (BF16 = false): the source is itself an MXFP8 row copy, src = its element bytes [rows x cols] (dense),
 // src_s = its scale bytes in the same layout as the outputs. Every value is decoded exactly on load and then
 // treated like an FP32 source: this derives the column copy of a tensor from its row copy (single-copy
 // storage, Section 5) at the price of a second rounding.
+// Rows (default: none): the source's rows are not consecutive; rows->load(r, c) gives VEC elements of row r of the tile from column c of
+// the tensor on, in the register layout of BF16, and src and ld_bytes are not looked at.
 // Tile (tile_y, tile_x) of the tensor by a workgroup of kQuantThreads work-items; the caller separates two tiles that use
 // the same LDS with a barrier.
-template <bool BF16, bool ROW, bool COL, bool TILED, int MODE, bool MXSRC = false>
+template <bool BF16, bool ROW, bool COL, bool TILED, int MODE, bool MXSRC = false, class Rows = NoRows>
 __device__ __forceinline__ void quantize_tile(
     const uint8_t *__restrict__ src, int64_t rows, int64_t cols, int64_t ld_bytes, uint8_t *__restrict__ q_row, uint8_t *__restrict__ s_row,
     uint8_t *__restrict__ q_colT, uint8_t *__restrict__ s_colT, const uint8_t *__restrict__ src_s, uint32_t tile_y, uint32_t tile_x, int tid,
-    const QuantLds &lds)
+    const QuantLds &lds, [[maybe_unused]] const Rows *source_rows = nullptr)
 {
     static_assert(!MXSRC || !BF16, "an MXFP8 source goes through the FP32 register layout");
     using T = QTraits<BF16>;
@@ -206,6 +212,9 @@ __device__ __forceinline__ void quantize_tile(
             if (active)
                 x[i] = decode_mx4(*reinterpret_cast<const uint32_t *>(lds_src + (lrow0 + i) * kTile + lcol0),
                                   (lds_src_s[lrow0 + i] >> (8 * (lcol0 / kBlock))) & 0xFFu);
+        } else if constexpr (Rows::kGiven) {
+            if (active)
+                x[i] = source_rows->load(lrow0 + i, col0);
         } else if (active) {
             x[i] = stream_load(reinterpret_cast<const uint4 *>(src + (row0 + i) * ld_bytes + col0 * ESIZE));
         }

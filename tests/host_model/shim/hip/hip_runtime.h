@@ -51,6 +51,12 @@ inline uint32_t __float_as_uint(float f)
 #define __shfl_xor(v, mask, width) ::wavesim::shfl_xor((v), (mask))
 #define __shfl(v, src, width) ::wavesim::shfl((v), (src))
 #define __ballot(b) ::wavesim::ballot(b)
+inline uint32_t atomicAdd(uint32_t *p, uint32_t v)  // one fiber runs at a time
+{
+    const uint32_t old = *p;
+    *p = old + v;
+    return old;
+}
 #define __popcll(v) __builtin_popcountll(v)
 
 #define __builtin_amdgcn_readfirstlane(x) ::wavesim::readfirstlane(x)
@@ -72,6 +78,7 @@ inline uint32_t __float_as_uint(float f)
     ::wavesim::cvt_scalef32_pk_fp4_f32((old), (a), (b), (scale), (sel))
 #define __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(old, p, scale, sel) \
     ::wavesim::cvt_scalef32_pk_fp4_bf16((old), (p), (scale), (sel))
+#define __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(q, scale, sel) ::wavesim::cvt_scalef32_pk_bf16_fp4((q), (scale), (sel))
 #define __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(old, a, b, scale, hi) \
     ::wavesim::cvt_scalef32_pk_bf8_f32((old), (a), (b), (scale), (hi))
 #define __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(old, p, scale, hi) \

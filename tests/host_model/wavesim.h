@@ -517,6 +517,22 @@ inline double e2m1_value(unsigned code)
     return (code & 8u) ? -mag : mag;
 }
 
+// v_cvt_scalef32_pk_bf16_fp4: the two codes of byte `sel` (low nibble first) times 2^(field - 127), same reading of the scale operand
+// as the narrowing forms, rounded to BF16 (RNE, subnormals kept); a NaN under a NaN scale.
+inline v2bf cvt_scalef32_pk_bf16_fp4(uint32_t q, float scale, int sel)
+{
+    uint32_t sbits;
+    memcpy(&sbits, &scale, 4);
+    const int field = (sbits >> 23) & 0xFF;
+    const uint32_t byte = (q >> (8 * sel)) & 0xFF;
+    v2bf r;
+    for (int i = 0; i < 2; ++i) {
+        const double v = e2m1_value((byte >> (4 * i)) & 15);
+        r[i] = field == 0xFF ? (__bf16)NAN : (__bf16)(float)std::ldexp(v, field == 0 ? -127 : field - 127);
+    }
+    return r;
+}
+
 // With both operands E2M1 (cbsz = blgp = 4) only dwords 0..3 are used: lane 16g+r holds K 32g..32g+31 of row r,
 // eight elements per dword, and its scale byte scales exactly those (K block g).
 // v_mfma_scale_f32_16x16x128_f8f6f4 with both operands E4M3: lane 16g+r holds row r of its operand,
