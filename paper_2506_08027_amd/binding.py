@@ -130,7 +130,9 @@ def _bind_fastcall(lib):
         return None
     table = {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "mxfp8_quantize_mode_ex", "mxfp8_gemm_ex", "mxfp8_gemm_mode_ex", "mxfp8_dequantize_mode_ex", "mxfp8_gemm_bf16",
-        "mxfp8_gemm_quantize_ex", "mxfp8_fp4_quantize_ex", "mxfp8_fp4_gemm_ex", "mxfp8_fp6_quantize_ex")}
+        "mxfp8_gemm_quantize_ex", "mxfp8_fp4_quantize_ex", "mxfp8_fp4_gemm_ex", "mxfp8_fp6_quantize_ex", "mxfp8_expert_sort",
+        "mxfp8_expert_sort_workspace", "mxfp8_expert_quantize_ex", "mxfp8_expert_combine", "mxfp8_expert_weight_grad", "mxfp8_fp4_gemv_ex",
+        "mxfp8_fp4_gemv_grouped_ex")}
     _fastcall.bind(dict(table, passes=_PASS, axes=_AXIS, stream=_stream))
     return _fastcall
 

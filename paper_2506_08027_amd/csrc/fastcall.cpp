@@ -7,19 +7,24 @@
 // The library's entry points are handed over by address, so that this module and the binding call the same library.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <initializer_list>
 
 namespace {
 
 constexpr long NOT_HANDLED = -1;
 constexpr int kRowwise = 1, kColwise = 2, kTiled = 1;
 // entry points, in the order of the names below
-enum { QUANTIZE, GEMM, GEMM_MODE, DEQUANTIZE, GEMM_BF16, GEMM_QUANTIZE, FP4_QUANTIZE, FP4_GEMM, FP6_QUANTIZE, ENTRY_POINTS };
+enum { QUANTIZE, GEMM, GEMM_MODE, DEQUANTIZE, GEMM_BF16, GEMM_QUANTIZE, FP4_QUANTIZE, FP4_GEMM, FP6_QUANTIZE, EXPERT_SORT, EXPERT_SORT_WORKSPACE,
+       EXPERT_QUANTIZE, EXPERT_COMBINE, EXPERT_WEIGHT_GRAD, FP4_GEMV, FP4_GEMV_GROUPED, ENTRY_POINTS };
 const char *const kNames[ENTRY_POINTS] = {"mxfp8_quantize_mode_ex", "mxfp8_gemm_ex", "mxfp8_gemm_mode_ex", "mxfp8_dequantize_mode_ex",
                                           "mxfp8_gemm_bf16", "mxfp8_gemm_quantize_ex", "mxfp8_fp4_quantize_ex",
-                                          "mxfp8_fp4_gemm_ex", "mxfp8_fp6_quantize_ex"};
+                                          "mxfp8_fp4_gemm_ex", "mxfp8_fp6_quantize_ex", "mxfp8_expert_sort", "mxfp8_expert_sort_workspace",
+                                          "mxfp8_expert_quantize_ex", "mxfp8_expert_combine", "mxfp8_expert_weight_grad", "mxfp8_fp4_gemv_ex",
+                                          "mxfp8_fp4_gemv_grouped_ex"};
 void *entry[ENTRY_POINTS];
 // The binding's own: names and constants of passes and axes (dicts), and the function that turns its `stream` argument into a handle.
 PyObject *passes, *axes, *stream_handle;
@@ -259,6 +264,142 @@ PyObject *gemm_quantize(PyObject *, PyObject *const *args, Py_ssize_t n)
         ptr(q.q_colT), ptr(q.s_colT), (int)layout, (int32_t)bound);
 }
 
+// ---- expert rows and products of a few rows (experts.py) ----------------------------------------------------------------
+// Whether all of them (nullptr: not given) are on the current device.
+bool on_current_device(std::initializer_list<const at::Tensor *> tensors)
+{
+    const auto current = c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice();
+    for (const at::Tensor *t : tensors)
+        if (t && t->device() != current)
+            return false;
+    return true;
+}
+bool numbers(const at::Tensor &t, int64_t n) { return t.scalar_type() == at::kInt && t.is_contiguous() && t.numel() == n; }
+bool weights_ok(const at::Tensor *t, int64_t n) { return !t || (t->scalar_type() == at::kFloat && t->is_contiguous() && t->numel() == n); }
+constexpr int64_t kMany = int64_t(1) << 30;
+
+// experts, align, positions, sources, group_ends, workspace, stream
+PyObject *expert_sort(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args a{args, n};
+    const at::Tensor *experts = a.tensor();
+    const int64_t align = a.number(1, INT32_MAX);
+    const at::Tensor *positions = a.tensor(), *sources = a.tensor(), *ends = a.tensor(), *workspace = a.tensor(true);
+    PyObject *stream = a.next();
+    if (!a.ok || a.left || !entry[EXPERT_SORT_WORKSPACE])
+        return not_handled();
+    const int64_t entries = experts->numel(), groups = ends->numel(), rows = sources->numel();
+    const bool wide = experts->scalar_type() == at::kLong;
+    if ((!wide && experts->scalar_type() != at::kInt) || !experts->is_contiguous() || entries > kMany || groups > INT32_MAX || !numbers(*positions, entries) ||
+        !numbers(*sources, rows) || !numbers(*ends, groups) || !on_current_device({experts, positions, sources, ends, workspace}))
+        return not_handled();
+    const int64_t need = reinterpret_cast<int64_t (*)(int64_t, int32_t)>(entry[EXPERT_SORT_WORKSPACE])(entries, (int32_t)groups);
+    if (need < 0 || (need > 0 && (!workspace || !workspace->is_contiguous() || (int64_t)workspace->nbytes() < need)))
+        return not_handled();
+    return call<int (*)(P, int, I, int32_t, int32_t, I, Q, Q, Q, Q, void *)>(EXPERT_SORT, stream, ptr(experts), wide ? 1 : 0, entries, (int32_t)groups,
+                                                                            (int32_t)align, rows, ptr(positions), ptr(sources), ptr(ends), ptr(workspace));
+}
+
+// src, sources, group_ends, slots, weights, axis, q_row, s_row, q_colT, s_colT, layout, stream
+PyObject *expert_quantize(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args a{args, n};
+    const at::Tensor *src = a.tensor(), *sources = a.tensor(), *ends = a.tensor(true);
+    const int64_t slots = a.number(1, 4096);
+    const at::Tensor *weights = a.tensor(true);
+    const int64_t axis = a.code(axes, 1, 3);
+    Copies c;
+    c.q_row = a.tensor(true);
+    c.s_row = a.tensor(true);
+    c.q_colT = a.tensor(true);
+    c.s_colT = a.tensor(true);
+    const int64_t layout = a.number(0, 1);
+    PyObject *stream = a.next();
+    if (!a.ok || a.left || src->dim() != 2)
+        return not_handled();
+    const int64_t tokens = src->size(0), cols = src->size(1), rows = sources->numel(), groups = ends ? ends->numel() : 0;
+    const Values v = values(*src, tokens, cols);
+    if (!v.ok || tokens > kMany || rows > kMany || rows % 32 || cols % 32 || !numbers(*sources, rows) || (ends && (groups == 0 || groups > 4096 || !numbers(*ends, groups))) ||
+        !weights_ok(weights, tokens * slots) || !copies(a, c, rows, cols, axis, layout, 1, 1) || ((axis & kRowwise) && !dense_matrix(*c.q_row, rows, cols)) ||
+        ((axis & kColwise) && !dense_matrix(*c.q_colT, cols, rows)) || !on_current_device({src, sources, ends, weights, c.q_row, c.s_row, c.q_colT, c.s_colT}))
+        return not_handled();
+    return call<int (*)(P, int, I, I, I, P, int32_t, P, P, int32_t, I, int, Q, Q, Q, Q, int, void *)>(
+        EXPERT_QUANTIZE, stream, ptr(src), v.dtype, tokens, cols, v.ld, ptr(sources), (int32_t)slots, ptr(weights), ptr(ends), (int32_t)groups, rows, (int)axis,
+        ptr(c.q_row), ptr(c.s_row), ptr(c.q_colT), ptr(c.s_colT), (int)layout);
+}
+
+// c, positions, weights, out, stream
+PyObject *expert_combine(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args a{args, n};
+    const at::Tensor *c = a.tensor(), *positions = a.tensor(), *weights = a.tensor(true), *out = a.tensor();
+    PyObject *stream = a.next();
+    if (!a.ok || a.left || c->dim() != 2 || positions->dim() != 2)
+        return not_handled();
+    const int64_t rows = c->size(0), cols = c->size(1), tokens = positions->size(0), slots = positions->size(1);
+    const Values v = values(*c, rows, cols), o = values(*out, tokens, cols);
+    if (!v.ok || !o.ok || tokens > kMany || slots > 4096 || !numbers(*positions, tokens * slots) || !weights_ok(weights, tokens * slots) ||
+        !on_current_device({c, positions, weights, out}))
+        return not_handled();
+    return call<int (*)(P, int, I, I, I, P, P, I, int32_t, Q, int, I, void *)>(EXPERT_COMBINE, stream, ptr(c), v.dtype, rows, cols, v.ld, ptr(positions), ptr(weights),
+                                                                              tokens, (int32_t)slots, ptr(out), o.dtype, o.ld);
+}
+
+// dy, c, positions, dweights, stream
+PyObject *expert_weight_grad(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args a{args, n};
+    const at::Tensor *dy = a.tensor(), *c = a.tensor(), *positions = a.tensor(), *dw = a.tensor();
+    PyObject *stream = a.next();
+    if (!a.ok || a.left || c->dim() != 2 || positions->dim() != 2)
+        return not_handled();
+    const int64_t rows = c->size(0), cols = c->size(1), tokens = positions->size(0), slots = positions->size(1);
+    const Values v = values(*c, rows, cols), d = values(*dy, tokens, cols);
+    if (!v.ok || !d.ok || tokens > kMany || slots > 4096 || !numbers(*positions, tokens * slots) || !weights_ok(dw, tokens * slots) ||
+        !on_current_device({dy, c, positions, dw}))
+        return not_handled();
+    return call<int (*)(P, int, I, P, int, I, I, I, P, I, int32_t, Q, void *)>(EXPERT_WEIGHT_GRAD, stream, ptr(dy), d.dtype, d.ld, ptr(c), v.dtype, rows, cols, v.ld,
+                                                                              ptr(positions), tokens, (int32_t)slots, ptr(dw));
+}
+
+// x, w_q, w_s, c, layout, stream
+PyObject *fp4_gemv(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args a{args, n};
+    const at::Tensor *x = a.tensor(), *w_q = a.tensor(), *w_s = a.tensor(), *c = a.tensor();
+    const int64_t layout = a.number(0, 1);
+    PyObject *stream = a.next();
+    if (!a.ok || a.left || x->dim() != 2 || w_q->dim() != 2)
+        return not_handled();
+    const int64_t M = x->size(0), K = x->size(1), N = w_q->size(0);
+    const Values v = values(*x, M, K), o = values(*c, M, N);
+    if (!v.ok || v.dtype != 1 || !o.ok || K % 32 || !dense_matrix(*w_q, N, K / 2) || !scales(*w_s, N, K, layout) || !on_current_device({x, w_q, w_s, c}))
+        return not_handled();
+    return call<int (*)(P, I, P, P, I, I, I, Q, int, I, int, void *)>(FP4_GEMV, stream, ptr(x), v.ld, ptr(w_q), ptr(w_s), M, N, K, ptr(c), o.dtype, o.ld, (int)layout);
+}
+
+// x, sources, slots, w_q, w_s, group_ends, c, layout, stream
+PyObject *fp4_gemv_grouped(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    Args a{args, n};
+    const at::Tensor *x = a.tensor(), *sources = a.tensor(true);
+    const int64_t slots = a.number(1, 4096);
+    const at::Tensor *w_q = a.tensor(), *w_s = a.tensor(), *ends = a.tensor(), *c = a.tensor();
+    const int64_t layout = a.number(0, 1);
+    PyObject *stream = a.next();
+    if (!a.ok || a.left || x->dim() != 2 || w_q->dim() != 3 || c->dim() != 2)
+        return not_handled();
+    const int64_t tokens = x->size(0), K = x->size(1), groups = w_q->size(0), N = w_q->size(1), M = c->size(0);
+    const Values v = values(*x, tokens, K), o = values(*c, M, N);
+    if (!v.ok || v.dtype != 1 || !o.ok || K % 32 || N > kMany || groups < 1 || groups > 4096 || w_q->size(2) != K / 2 || !dense_bytes(*w_q) || !dense_bytes(*w_s) ||
+        w_s->numel() != groups * (layout == kTiled ? (N + 63) / 64 * ((K / 32 + 3) / 4) * 256 : N * (K / 32)) || !numbers(*ends, groups) ||
+        (sources ? !numbers(*sources, M) : tokens < M) || !on_current_device({x, sources, w_q, w_s, ends, c}))
+        return not_handled();
+    return call<int (*)(P, I, I, P, int32_t, P, P, P, int32_t, I, I, I, Q, int, I, int, void *)>(FP4_GEMV_GROUPED, stream, ptr(x), tokens, v.ld, ptr(sources),
+                                                                                                 (int32_t)slots, ptr(w_q), ptr(w_s), ptr(ends), (int32_t)groups, M, N,
+                                                                                                 K, ptr(c), o.dtype, o.ld, (int)layout);
+}
+
 // {name: address} of the entry points, and the binding's "passes", "axes" and "stream"
 PyObject *bind(PyObject *, PyObject *table)
 {
@@ -302,7 +443,9 @@ template <PyObject *(*FN)(PyObject *, PyObject *const *, Py_ssize_t)> PyObject *
 #define FAST(name, ...) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<__VA_ARGS__>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST("quantize", quantize<QUANTIZE>), FAST("fp4_quantize", quantize<FP4_QUANTIZE>), FAST("fp6_quantize", quantize<FP6_QUANTIZE>),
                          FAST("gemm", gemm<GEMM>), FAST("gemm_mode", gemm<GEMM_MODE>), FAST("fp4_gemm", gemm<FP4_GEMM>), FAST("dequantize", dequantize),
-                         FAST("gemm_bf16", gemm_bf16), FAST("gemm_quantize", gemm_quantize), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         FAST("gemm_bf16", gemm_bf16), FAST("gemm_quantize", gemm_quantize), FAST("expert_sort", expert_sort),
+                         FAST("expert_quantize", expert_quantize), FAST("expert_combine", expert_combine), FAST("expert_weight_grad", expert_weight_grad),
+                         FAST("fp4_gemv", fp4_gemv), FAST("fp4_gemv_grouped", fp4_gemv_grouped), {"bind", bind, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

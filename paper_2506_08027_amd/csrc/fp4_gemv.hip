@@ -1,21 +1,26 @@
 // Products of a few rows of BF16 activations with MXFP4 weights (include/mxfp8_experts.h): C[m, n] = sum_k x[m, k] W[n, k].
 //
-// Every weight is read once for up to 16 rows of x, so HBM is the bound as long as the matrix and LDS work hide behind it. A workgroup
-// has 16 rows of W and all of K, its wavefronts take turns at K and their sums are joined in LDS. The 4-bit codes
-// are widened to BF16, scale included, by v_cvt_scalef32_pk_bf16_fp4 (exact where BF16 holds the value), and multiplied on
-// v_mfma_f32_16x16x32_bf16. That instruction takes 8 consecutive k a lane, but any order of k will do that x and W share: lane 16g + r
-// loads the 16 bytes of block 4u + g of weight row r, a whole scale block, and instruction i of four takes their elements
-// 8i .. 8i + 7; the lane's scale byte applies to all of them.
+// Every weight is read once for up to 64 rows of x, so HBM is the bound as long as all else hides behind it. A wavefront takes 16 rows of
+// W and a contiguous part of K, in units of 128 k: the 4-bit codes are widened to BF16, scale included, by
+// v_cvt_scalef32_pk_bf16_fp4 (exact where BF16 holds the value) and multiplied on v_mfma_f32_16x16x32_bf16, W as its first operand. Where a
+// workgroup's wavefronts share rows of W, their sums are joined in LDS in a fixed order; until then no wavefront waits for another.
+//   Layout. The instruction takes 8 consecutive k a lane, but any order of k will do that x and W share: lane 16g + r has block g of a unit of
+//   weight row r, a whole scale block, and instruction i of four multiplies its elements 8i .. 8i + 7. Loaded in that order, neighbouring lanes
+//   would read different rows and a load would take four times its time in the address unit (measured: x and W read in place, [12 x 4096 x
+//   14336] 17.4 us). So four neighbouring lanes load 64 bytes of a row of W and 16 lanes 256 bytes of a row of x, and each
+//   wavefront reorders them through an LDS area of its own. Rows that are not there are read from one that is, and their column of the
+//   result is dropped: a load under a condition would have to be waited for before the loads behind it.
 #include "expert_launches.h"
 #include "gemm_device.h"
 
+#include <type_traits>
+
 namespace mxfp8 {
 
-constexpr int kUnit = 4;            // scale blocks of a unit: 128 k, 64 bytes of a weight row
+constexpr int kUnit = 4;  // scale blocks of a unit: 128 k, 64 bytes of a weight row, 256 bytes of a row of x
 constexpr int kGemvWaves = 8, kGemvThreads = 64 * kGemvWaves;
-constexpr int kXLds = 64 * 1024;    // LDS for the activations
 
-// two bytes of E2M1 codes -> ... eight codes of a word as BF16, times the scale
+// the eight codes of a word as BF16, times the scale
 __device__ __forceinline__ v8bf fp4_word_bf16(uint32_t w, float scale)
 {
     const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1),
@@ -37,39 +42,46 @@ struct GemvPiece {
 };
 template <int R> __device__ __forceinline__ GemvPiece grouped_piece(const int32_t *__restrict__ ends, int groups, int M, int u, int lane)
 {
-    int before = 0;  // pieces of the experts before e0
+    int before = 0, last_end = 0;  // pieces of the experts before e0, and the end of the last of them
     for (int e0 = 0; e0 < groups; e0 += 64) {
         const int e = e0 + lane;
-        const int end = e < groups ? min(max(ends[e], 0), M) : 0, begin = e < groups && e > 0 ? min(max(ends[e - 1], 0), M) : 0;
-        const int rows = max(end - begin, 0), n = (rows + R - 1) / R;
-        int upto = n;
-        for (int d = 1; d < 64; d *= 2) {
-            const int o = __shfl(upto, lane >= d ? lane - d : lane, 64);
-            upto += lane >= d ? o : 0;
-        }
+        const int end = e < groups ? min(max(ends[e], 0), M) : 0;
+        const int prev = __shfl(end, max(lane - 1, 0), 64), begin = lane == 0 ? last_end : prev;
+        const int rows = e < groups ? max(end - begin, 0) : 0, n = (rows + R - 1) / R;
+        int upto = n;  // inclusive sum: over the rows of 16 lanes, then over those
+        upto += (int)__builtin_amdgcn_update_dpp(0, upto, 0x111, 0xF, 0xF, true);
+        upto += (int)__builtin_amdgcn_update_dpp(0, upto, 0x112, 0xF, 0xF, true);
+        upto += (int)__builtin_amdgcn_update_dpp(0, upto, 0x114, 0xF, 0xF, true);
+        upto += (int)__builtin_amdgcn_update_dpp(0, upto, 0x118, 0xF, 0xF, true);
+        const int s0 = __builtin_amdgcn_readlane(upto, 15), s1 = s0 + __builtin_amdgcn_readlane(upto, 31), s2 = s1 + __builtin_amdgcn_readlane(upto, 47);
+        upto += lane < 16 ? 0 : lane < 32 ? s0 : lane < 48 ? s1 : s2;
         const uint64_t past = __ballot(before + upto > u);
         if (past) {
             const int l = __builtin_ctzll(past);
-            const int k = u - before - (__shfl(upto, l, 64) - __shfl(n, l, 64));
-            return {e0 + l, __shfl(begin, l, 64) + k * R, min(__shfl(rows, l, 64) - k * R, R)};
+            const int k = u - before - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
+            return {e0 + l, __builtin_amdgcn_readlane(begin, l) + k * R, min(__builtin_amdgcn_readlane(rows, l) - k * R, R)};
         }
-        before += __shfl(upto, 63, 64);
+        before += __builtin_amdgcn_readlane(upto, 63);
+        last_end = __builtin_amdgcn_readlane(end, 63);
     }
     return {0, 0, 0};
 }
 
-// MT tiles of 16 rows of x. x in LDS: [unit][row][16 pieces of 16 bytes], piece 4g + i at place (4g + i) ^ (row & 15), so that the
-// sixteen rows that a fragment read touches lie in different banks.
-template <int MT, bool TILED, bool GROUPED>
+// XR rows of x (up to 16, or a multiple of it); WK wavefronts along K, the others along N. U units (4, 2 or 1) are loaded at a time.
+template <int XR, int WK, int U, bool TILED, bool GROUPED>
 __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *__restrict__ x, int64_t ldx_bytes, GemvRows map,
                                                                 const uint8_t *__restrict__ w_q, const uint8_t *__restrict__ w_s, int M, int N, int nb,
-                                                                uint32_t tiles_n, uint8_t *__restrict__ c, bool c_bf16, int64_t ldc, bool c_vector)
+                                                                uint32_t blocks_n, uint8_t *__restrict__ c, bool c_bf16, int64_t ldc, bool c_vector)
 {
-    MXFP8_DYNAMIC_LDS(lds);
-    __shared__ int64_t x_row[MT * 16];  // byte offset of a row of x, -1: zeros
-    constexpr int R = MT * 16;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4;
-    const uint32_t tile = blockIdx.x % tiles_n, u_piece = blockIdx.x / tiles_n;
+    constexpr int R = XR, MT = (XR + 15) / 16, WN = kGemvWaves / WK;
+    constexpr int LANES = 16 * U;             // lanes of a row of x in a load
+    constexpr int XL = XR * LANES > 64 ? XR * LANES / 64 : 1;  // loads of x
+    // LDS of a wavefront, in pieces of 16 bytes: x [row][unit][16], W [unit][row][4], scales [row] (the dwords of four units)
+    constexpr int XP = XR * LANES > 64 ? XR * LANES : 64, WP = U * 64;
+    __shared__ uint4 staged[kGemvWaves][XP + WP + 16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int wk = wave % WK, wn = wave / WK;
+    const uint32_t block = blockIdx.x % blocks_n, u_piece = blockIdx.x / blocks_n;
     GemvPiece p;
     if constexpr (GROUPED)
         p = grouped_piece<R>(map.ends, map.groups, M, (int)u_piece, lane);
@@ -77,126 +89,218 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
         p = {0, (int)u_piece * R, min(M - (int)u_piece * R, R)};
     if (p.count <= 0)
         return;
-    if (tid < p.count) {
-        const int row = p.first + tid;
-        int64_t at = row;
-        if (GROUPED && map.sources) {
-            const uint32_t i = (uint32_t)map.sources[row];
-            at = i < map.entries ? (int64_t)(i / map.slots) : -1;
+
+    // ---- rows of x of the columns that this lane has of C (-1: zeros), and of the pieces that it loads
+    int at[MT];
+    uint64_t any = 0;
+    int first_row = 0;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        at[t] = t * 16 + r < p.count ? p.first + t * 16 + r : -1;
+        if (GROUPED && map.sources && at[t] >= 0) {
+            const uint32_t i = (uint32_t)map.sources[at[t]];
+            at[t] = i < map.entries ? (int)(i / map.slots) : -1;
         }
-        x_row[tid] = at < 0 ? -1 : at * ldx_bytes;
+        const uint64_t given = __ballot(at[t] >= 0);
+        if (!any && given)
+            first_row = __builtin_amdgcn_readlane(at[t], (int)__builtin_ctzll(given));
+        any |= given;
     }
-    const int units = (nb + kUnit - 1) / kUnit;
-    // rows of x in LDS: a power of two; units that fit beside each other
-    int held = 1;
-    while (held < p.count)
-        held *= 2;
-    const int held_log = 31 - __builtin_clz((unsigned)held), chunk = kXLds / 256 >> held_log;
+    const int lane_row = lane / LANES, lane_piece = lane % LANES;
+    const uint8_t *xp[XL];
+#pragma unroll
+    for (int q = 0; q < XL; ++q) {
+        const int m = q * (64 / LANES);  // the first of the rows of load q; they lie in one tile
+        const int row = U == 4 ? __builtin_amdgcn_readlane(at[m / 16], m % 16) : __shfl(at[m / 16], (m + lane_row) % 16, 64);
+        xp[q] = x + (row < 0 ? first_row : row) * ldx_bytes + lane_piece * 16;
+    }
+    // ---- rows of W: four lanes a row, from block 4u + lane % 4 on; scales of the next four units, one dword a lane
+    const int n0 = ((int)block * WN + wn) * 16;
+    const int w_row = min(n0 + (lane >> 2), N - 1), s_unit = TILED ? g : lane & 3, s_row = TILED ? r : lane >> 2, s_n = min(n0 + s_row, N - 1);
+    const uint8_t *const wq = w_q + p.expert * (GROUPED ? map.wq_group_bytes : 0) + w_row * ((int64_t)nb * 16) + (lane & 3) * 16;
+    const uint8_t *const ws = w_s + p.expert * (GROUPED ? map.ws_group_bytes : 0) +
+                              (TILED ? ((int64_t)(s_n >> 6) * ((nb + 3) / 4) * 64 + (s_n & 63)) * 4 : (int64_t)s_n * nb);
 
-    const int n0 = (int)tile * 16, wrow = min(n0 + r, N - 1);
-    const int64_t k_bytes = (int64_t)nb * 16;
-    const uint8_t *wq = w_q + p.expert * (GROUPED ? map.wq_group_bytes : 0) + wrow * k_bytes;
-    const uint8_t *ws = w_s + p.expert * (GROUPED ? map.ws_group_bytes : 0);
-    ws += TILED ? ((int64_t)(wrow >> 6) * ((nb + 3) / 4) * 64 + (wrow & 63)) * 4 : (int64_t)wrow * nb;
-
+    struct Units {
+        uint4 w[U], x[XL];
+        uint32_t s;
+    };
+    uint4 *const lds_x = staged[wave], *const lds_w = lds_x + XP;
+    uint32_t *const lds_s = reinterpret_cast<uint32_t *>(lds_w + WP);
     v4f acc[MT] = {};
-    for (int c0 = 0; c0 < units; c0 += chunk) {
-        const int here = min(chunk, units - c0);
-        __syncthreads();  // x_row is there; the last chunk has been read
-        const int pieces = here * 16;
-        for (int m = 0; m < p.count; ++m) {
-            const int64_t row = x_row[m];
-            for (int q = tid; q < pieces; q += kGemvThreads) {
-                const int unit = q >> 4, piece = q & 15;
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (row >= 0 && (c0 + unit) * kUnit + (piece >> 2) < nb)
-                    v = *reinterpret_cast<const uint4 *>(x + row + (int64_t)c0 * 256 + q * 16);
-                *reinterpret_cast<uint4 *>(lds + ((unit * held + m) * 16 + (piece ^ (m & 15))) * 16) = v;
-            }
+    const int units = any ? nb / kUnit : 0;  // whole ones
+    const int begin = (int)((int64_t)units * wk / WK), end = (int)((int64_t)units * (wk + 1) / WK);
+    auto load = [&](Units &d, int u) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            d.w[j] = stream_load(reinterpret_cast<const uint4 *>(wq + (int64_t)min(u + j, end - 1) * 64));
+        __builtin_memcpy(&d.s, ws + (int64_t)min(u + s_unit, end - 1) * (TILED ? 256 : 4), 4);
+        const int last = (end - u) * 16 - 1;  // pieces of x behind the last unit are not multiplied: any others will do
+#pragma unroll
+        for (int q = 0; q < XL; ++q)
+            d.x[q] = *reinterpret_cast<const uint4 *>(xp[q] + (int64_t)u * 256 + (lane_piece <= last ? 0 : -(lane_piece & ~15) * 16));
+        MXFP8_PIN();
+    };
+    // Places are XORed so that the sixteen lanes that are served together hit different banks.
+    auto multiply_units = [&](const Units &d, int count) __attribute__((always_inline)) {
+        MXFP8_FENCE();
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int q = 0; q < XL; ++q) {
+            const int m = q * (64 / LANES) + lane_row;
+            if (XR * LANES >= 64 || m < XR)
+                lds_x[m * LANES + (lane_piece ^ (m & 15))] = d.x[q];
         }
-        __syncthreads();
-        for (int u = wave; u < here; u += kGemvWaves) {
-            const int b = (c0 + u) * kUnit + g;  // this lane's block; blocks past the end are zeros
-            const bool there = b < nb;
-            uint4 w = make_uint4(0, 0, 0, 0);
-            uint32_t sb = 127;
-            if (there) {
-                w = *reinterpret_cast<const uint4 *>(wq + (int64_t)b * 16);
-                sb = TILED ? ws[(int64_t)(b >> 2) * 256 + (b & 3)] : ws[b];
-            }
-            const float scale = scale_operand(sb);
-            const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+            lds_w[j * 64 + (lane & ~3) + ((lane ^ (lane >> 4)) & 3)] = d.w[j];
+        lds_s[s_row * 4 + s_unit] = d.s;
+        __builtin_amdgcn_wave_barrier();
+        MXFP8_FENCE();
+        const uint4 scales = *reinterpret_cast<const uint4 *>(lds_s + r * 4);
+        const uint32_t s[4] = {scales.x, scales.y, scales.z, scales.w};
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            if (j >= count)
+                break;
+            const uint4 w4 = lds_w[j * 64 + r * 4 + (g ^ (r >> 2))];
+            const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+            const float scale = scale_operand((s[j] >> (8 * g)) & 0xFFu);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const v8bf a = fp4_word_bf16(words[i], scale);
+                const v8bf a = fp4_word_bf16(w[i], scale);
 #pragma unroll
                 for (int t = 0; t < MT; ++t) {
-                    const int m = min(t * 16 + r, held - 1);
-                    const v4i f = *reinterpret_cast<const v4i *>(lds + ((u * held + m) * 16 + ((4 * g + i) ^ (m & 15))) * 16);
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(v8bf, f), acc[t], 0, 0, 0);
+                    const int m = min(t * 16 + r, XR - 1);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(v8bf, lds_x[m * LANES + ((j * 16 + 4 * g + i) ^ (m & 15))]), acc[t],
+                                                                     0, 0, 0);
                 }
             }
         }
+        MXFP8_PIN();
+    };
+    for (int u = begin; u < end; u += U) {
+        Units d;
+        load(d, u);
+        multiply_units(d, end - u);
+    }
+    if (any && nb % kUnit && wk == WK - 1) {  // one to three blocks behind the whole units
+        const int rest = nb % kUnit;
+        Units d = {};
+        if ((lane & 3) < rest)
+            d.w[0] = *reinterpret_cast<const uint4 *>(wq + (int64_t)units * 64);
+        if (s_unit == 0)
+            for (int b = 0; b < rest; ++b)
+                d.s |= (uint32_t)ws[(int64_t)units * (TILED ? 256 : 4) + b] << (8 * b);
+        if (lane_piece < rest * 4)
+#pragma unroll
+            for (int q = 0; q < XL; ++q)
+                d.x[q] = *reinterpret_cast<const uint4 *>(xp[q] + (int64_t)units * 256);
+        multiply_units(d, 1);
     }
 
-    // ---- the wavefronts' sums, in their order
-    __syncthreads();
-    v4f *const sums = reinterpret_cast<v4f *>(lds);
+    // ---- sums of the wavefronts along K, in their order; wavefront k of them then stores the tiles k, k + WK, ...
+    if constexpr (WK > 1) {
+        static_assert(MT * 64 <= XP + WP, "the sums take the place of what is staged");
+        MXFP8_FENCE();
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
-        sums[(wave * MT + t) * 64 + lane] = acc[t];
-    __syncthreads();
-    if (wave >= MT)
-        return;
-    v4f sum = sums[wave * 64 + lane];
-    for (int w = 1; w < kGemvWaves; ++w)
-        sum += sums[(w * MT + wave) * 64 + lane];
-    const int m = wave * 16 + r, n = n0 + 4 * g;
-    if (m >= p.count || n >= N)
-        return;
-    uint8_t *const to = c + ((p.first + m) * ldc + n) * (c_bf16 ? 2 : 4);
-    if (c_bf16) {
-        const v2bf a = {(__bf16)sum[0], (__bf16)sum[1]}, b = {(__bf16)sum[2], (__bf16)sum[3]};
-        const uint2 h = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
-        if (c_vector && n + 4 <= N) {
-            *reinterpret_cast<uint2 *>(to) = h;
+        for (int t = 0; t < MT; ++t)
+            reinterpret_cast<v4f *>(staged[wave])[t * 64 + lane] = acc[t];
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+            if (t % WK == wk) {
+                acc[t] = reinterpret_cast<const v4f *>(staged[wn * WK])[t * 64 + lane];
+#pragma unroll
+                for (int k = 1; k < WK; ++k)
+                    acc[t] += reinterpret_cast<const v4f *>(staged[wn * WK + k])[t * 64 + lane];
+            }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int m = t * 16 + r, n = n0 + 4 * g;
+        if ((WK > 1 && t % WK != wk) || m >= p.count || n >= N)
+            continue;
+        const v4f sum = GROUPED && at[t] < 0 ? v4f{0, 0, 0, 0} : acc[t];
+        uint8_t *const to = c + ((p.first + m) * ldc + n) * (c_bf16 ? 2 : 4);
+        if (c_bf16) {
+            const v2bf a = {(__bf16)sum[0], (__bf16)sum[1]}, b = {(__bf16)sum[2], (__bf16)sum[3]};
+            const uint2 h = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+            if (c_vector && n + 4 <= N) {
+                *reinterpret_cast<uint2 *>(to) = h;
+            } else {
+                for (int v = 0; v < 4 && n + v < N; ++v)
+                    reinterpret_cast<uint16_t *>(to)[v] = (uint16_t)((v < 2 ? h.x : h.y) >> (16 * (v & 1)));
+            }
         } else {
-            for (int v = 0; v < 4 && n + v < N; ++v)
-                reinterpret_cast<uint16_t *>(to)[v] = (uint16_t)((v < 2 ? h.x : h.y) >> (16 * (v & 1)));
-        }
-    } else {
-        if (c_vector && n + 4 <= N) {
-            *reinterpret_cast<v4f *>(to) = sum;
-        } else {
-            for (int v = 0; v < 4 && n + v < N; ++v)
-                reinterpret_cast<float *>(to)[v] = sum[v];
+            if (c_vector && n + 4 <= N) {
+                *reinterpret_cast<v4f *>(to) = sum;
+            } else {
+                for (int v = 0; v < 4 && n + v < N; ++v)
+                    reinterpret_cast<float *>(to)[v] = sum[v];
+            }
         }
     }
+}
+
+// Pieces of at most R rows that the rows of C are cut into: an expert's rows take at most one more than they fill.
+static int64_t gemv_pieces(const GemvRows &map, int64_t M, int R)
+{
+    const int64_t some = map.ends ? min((int64_t)map.groups, M) : 0;
+    return map.ends ? some + (M - some) / R : (M + R - 1) / R;
+}
+
+template <int XR, int WK, int U, bool TILED>
+static hipError_t launch_fp4_gemv_t(const void *x, int64_t ldx, const GemvRows &map, const uint8_t *w_q, const uint8_t *w_s, int64_t M, int64_t N,
+                                    int64_t K, void *c, bool c_bf16, int64_t ldc, hipStream_t stream)
+{
+    constexpr int COLS = kGemvWaves / WK * 16;  // rows of W of a workgroup
+    const int64_t pieces = gemv_pieces(map, M, XR);
+    const int64_t blocks_n = (N + COLS - 1) / COLS;
+    if (blocks_n * pieces > 0x7FFFFFFF)
+        return hipErrorInvalidConfiguration;
+    const bool vector = reinterpret_cast<uintptr_t>(c) % 16 == 0 && (ldc * (c_bf16 ? 2 : 4)) % 16 == 0;
+    auto kern = map.ends ? fp4_gemv_kernel<XR, WK, U, TILED, true> : fp4_gemv_kernel<XR, WK, U, TILED, false>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(blocks_n * pieces)), dim3(kGemvThreads), 0, stream, static_cast<const uint8_t *>(x), ldx * 2, map, w_q, w_s,
+                       (int)M, (int)N, (int)(K / kBlock), (uint32_t)blocks_n, static_cast<uint8_t *>(c), c_bf16, ldc, vector);
+    return hipGetLastError();
+}
+
+template <int XR, int U, bool TILED>
+static hipError_t launch_fp4_gemv_rows(const void *x, int64_t ldx, const GemvRows &map, const uint8_t *w_q, const uint8_t *w_s, int64_t M, int64_t N,
+                                       int64_t K, void *c, bool c_bf16, int64_t ldc, hipStream_t stream)
+{
+    // As many wavefronts along K as have four units each, up to some 8192 in all.
+    const int64_t tiles = (N + 15) / 16 * gemv_pieces(map, M, XR), units = K / (kUnit * kBlock);
+    int wk = 1;
+    while (wk < kGemvWaves && units >= 8 * wk && tiles * wk * 2 <= 8192)
+        wk *= 2;
+    auto launch = wk == 1   ? launch_fp4_gemv_t<XR, 1, U, TILED>
+                  : wk == 2 ? launch_fp4_gemv_t<XR, 2, U, TILED>
+                  : wk == 4 ? launch_fp4_gemv_t<XR, 4, U, TILED>
+                            : launch_fp4_gemv_t<XR, 8, U, TILED>;
+    return launch(x, ldx, map, w_q, w_s, M, N, K, c, c_bf16, ldc, stream);
 }
 
 hipError_t launch_fp4_gemv(const void *x, int64_t tokens, int64_t ldx, const int32_t *sources, int slots, const uint8_t *w_q, const uint8_t *w_s,
                            const int32_t *group_ends, int groups, int64_t ws_group_bytes, int64_t M, int64_t N, int64_t K, void *c, bool c_bf16,
                            int64_t ldc, bool tiled_scales, hipStream_t stream)
 {
-    const bool grouped = group_ends != nullptr;
-    const int64_t rows = grouped ? (M + groups - 1) / groups : M;  // of a matrix, in the mean
-    const int mt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, R = 16 * mt;
-    // an expert's rows take at most one piece more than they fill
-    const int64_t some = grouped ? min((int64_t)groups, M) : 0, pieces = grouped ? some + (M - some) / R : (M + R - 1) / R;
-    const int64_t tiles_n = (N + 15) / 16, workgroups = tiles_n * pieces;
-    if (workgroups > 0x7FFFFFFF)
-        return hipErrorInvalidConfiguration;
     const GemvRows map = {sources, (uint32_t)(tokens * slots), (uint32_t)slots, group_ends, groups, N * (K / 2), ws_group_bytes};
-    const int64_t es = c_bf16 ? 2 : 4;
-    const bool vector = reinterpret_cast<uintptr_t>(c) % 16 == 0 && (ldc * es) % 16 == 0;
-    auto pick = [&](auto one, auto two, auto four) { return mt == 1 ? one : mt == 2 ? two : four; };
-    auto kern = grouped ? (tiled_scales ? pick(fp4_gemv_kernel<1, true, true>, fp4_gemv_kernel<2, true, true>, fp4_gemv_kernel<4, true, true>)
-                                        : pick(fp4_gemv_kernel<1, false, true>, fp4_gemv_kernel<2, false, true>, fp4_gemv_kernel<4, false, true>))
-                        : (tiled_scales ? pick(fp4_gemv_kernel<1, true, false>, fp4_gemv_kernel<2, true, false>, fp4_gemv_kernel<4, true, false>)
-                                        : pick(fp4_gemv_kernel<1, false, false>, fp4_gemv_kernel<2, false, false>, fp4_gemv_kernel<4, false, false>));
-    hipLaunchKernelGGL(kern, dim3((unsigned)workgroups), dim3(kGemvThreads), kXLds, stream, static_cast<const uint8_t *>(x), ldx * 2, map, w_q, w_s,
-                       (int)M, (int)N, (int)(K / kBlock), (uint32_t)tiles_n, static_cast<uint8_t *>(c), c_bf16, ldc, vector);
-    return hipGetLastError();
+    // Rows that an expert is made ready for: what it has in the mean is known, and the ones that are chosen have more than that.
+    const int64_t rows = !group_ends ? M : M == 1 || (sources && tokens == 1) ? 1 : (M + groups - 1) / groups * 3 / 2 + 1;
+    auto launch = [&](auto tiled) {
+        constexpr bool T = decltype(tiled)::value;
+        auto pick = rows <= 1    ? launch_fp4_gemv_rows<1, 4, T>
+                    : rows <= 4  ? launch_fp4_gemv_rows<4, 4, T>
+                    : rows <= 8  ? launch_fp4_gemv_rows<8, 2, T>
+                    : rows <= 16 ? launch_fp4_gemv_rows<16, 2, T>
+                    : rows <= 32 ? launch_fp4_gemv_rows<32, 1, T>
+                                 : launch_fp4_gemv_rows<64, 1, T>;
+        return pick(x, ldx, map, w_q, w_s, M, N, K, c, c_bf16, ldc, stream);
+    };
+    return tiled_scales ? launch(std::true_type{}) : launch(std::false_type{});
 }
 
 }  // namespace mxfp8

@@ -41,9 +41,14 @@ def _matrix(t, what, rows=None, cols=None):
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-def _done(rc, what):
+def _check_status(rc, what):
     if rc != OK:
         raise MXFP8Error(rc, what)
+
+
+def _fast(name, what, *args) -> bool:
+    """Whether the call of that name in C++ (csrc/fastcall.cpp) did it all."""
+    return _b._fast is not None and _b._done(getattr(_b._fast, name)(*args), what)
 
 
 # ---- raw entry points: same names and argument order as include/mxfp8_experts.h ------------------------------------------
@@ -67,6 +72,8 @@ def mxfp8_expert_sort_workspace(entries: int, groups: int) -> int:
 def mxfp8_expert_sort(experts, align, positions, sources, group_ends, workspace=None, stream=None) -> None:
     """experts int32/int64 [tokens x slots] -> positions (int32, as many), sources (int32 [rows]), group_ends (int32 [groups]).
     workspace: uint8 of mxfp8_expert_sort_workspace(entries, groups) bytes, None where that is 0."""
+    if _fast("expert_sort", "mxfp8_expert_sort", experts, align, positions, sources, group_ends, workspace, stream):
+        return
     _ready(experts, positions, sources, group_ends, workspace)
     if experts.dtype not in (torch.int32, torch.int64) or not experts.is_contiguous():
         raise ValueError("experts must be contiguous int32 or int64")
@@ -77,7 +84,7 @@ def mxfp8_expert_sort(experts, align, positions, sources, group_ends, workspace=
     need = mxfp8_expert_sort_workspace(entries, groups)
     if need and (workspace is None or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need):
         raise ValueError(f"the sort of {entries} entries to {groups} experts needs a contiguous workspace of {need} bytes")
-    _done(_b.load().mxfp8_expert_sort(_b._ptr(experts), I64 if experts.dtype == torch.int64 else I32, entries, groups, align, sources.numel(),
+    _check_status(_b.load().mxfp8_expert_sort(_b._ptr(experts), I64 if experts.dtype == torch.int64 else I32, entries, groups, align, sources.numel(),
                                       _b._ptr(positions), _b._ptr(sources), _b._ptr(group_ends), _b._ptr(workspace), _b._stream(stream)),
           "mxfp8_expert_sort")
 
@@ -86,6 +93,8 @@ def mxfp8_expert_quantize_ex(src, sources, group_ends, slots, weights, axis, q_r
                              scale_layout=SCALES_ROWMAJOR, stream=None) -> None:
     """MXFP8 copies of the sorted rows weights[i] * src[i // slots] with i = sources[r], zeros for -1. src [tokens x cols]
     float32/bfloat16; weights float32 [tokens x slots] or None; group_ends int32, or None to convert all rows."""
+    if _fast("expert_quantize", "mxfp8_expert_quantize_ex", src, sources, group_ends, slots, weights, axis, q_row, s_row, q_colT, s_colT, scale_layout, stream):
+        return
     _ready(src, sources, group_ends, weights, q_row, s_row, q_colT, s_colT)
     ld = _matrix(src, "src")
     tokens, cols = src.shape
@@ -104,7 +113,7 @@ def mxfp8_expert_quantize_ex(src, sources, group_ends, slots, weights, axis, q_r
             if q is None or s is None or q.dtype != torch.uint8 or not q.is_contiguous() or tuple(q.shape) != shape:
                 raise ValueError(f"q_{name} must be dense uint8 [{shape[0]} x {shape[1]}], s_{name} its scales")
             _b._check_scales(s, *shape, scale_layout, f"s_{name}")
-    _done(_b.load().mxfp8_expert_quantize_ex(_b._ptr(src), _b._dtype_code(src.dtype), tokens, cols, ld, _b._ptr(sources), slots, _b._ptr(weights),
+    _check_status(_b.load().mxfp8_expert_quantize_ex(_b._ptr(src), _b._dtype_code(src.dtype), tokens, cols, ld, _b._ptr(sources), slots, _b._ptr(weights),
                                              _b._ptr(group_ends), 0 if group_ends is None else group_ends.numel(), rows, ax, _b._ptr(q_row),
                                              _b._ptr(s_row), _b._ptr(q_colT), _b._ptr(s_colT), scale_layout, _b._stream(stream)),
           "mxfp8_expert_quantize_ex")
@@ -113,6 +122,8 @@ def mxfp8_expert_quantize_ex(src, sources, group_ends, slots, weights, axis, q_r
 def mxfp8_expert_combine(c, positions, weights, out, stream=None) -> None:
     """out [tokens x cols] = sum over slots of weights * c[positions] (None: plain sum). c [rows x cols], positions int32
     [tokens x slots], -1 adds nothing; weights float32 of the same shape."""
+    if _fast("expert_combine", "mxfp8_expert_combine", c, positions, weights, out, stream):
+        return
     _ready(c, positions, weights, out)
     ldc = _matrix(c, "c")
     rows, cols = c.shape
@@ -122,12 +133,14 @@ def mxfp8_expert_combine(c, positions, weights, out, stream=None) -> None:
     _check_index(positions, None, "positions")
     _check_weights(weights, tokens * slots)
     ld_out = _matrix(out, "out", tokens, cols)
-    _done(_b.load().mxfp8_expert_combine(_b._ptr(c), _b._dtype_code(c.dtype), rows, cols, ldc, _b._ptr(positions), _b._ptr(weights), tokens, slots,
+    _check_status(_b.load().mxfp8_expert_combine(_b._ptr(c), _b._dtype_code(c.dtype), rows, cols, ldc, _b._ptr(positions), _b._ptr(weights), tokens, slots,
                                          _b._ptr(out), _b._dtype_code(out.dtype), ld_out, _b._stream(stream)), "mxfp8_expert_combine")
 
 
 def mxfp8_expert_weight_grad(dy, c, positions, dweights, stream=None) -> None:
     """dweights float32 [tokens x slots] = dot products of dy [tokens x cols] with the rows c[positions], 0 for -1."""
+    if _fast("expert_weight_grad", "mxfp8_expert_weight_grad", dy, c, positions, dweights, stream):
+        return
     _ready(dy, c, positions, dweights)
     ldc = _matrix(c, "c")
     rows, cols = c.shape
@@ -138,7 +151,7 @@ def mxfp8_expert_weight_grad(dy, c, positions, dweights, stream=None) -> None:
     ld_dy = _matrix(dy, "dy", tokens, cols)
     if dweights.dtype != torch.float32 or not dweights.is_contiguous() or dweights.numel() != tokens * slots:
         raise ValueError(f"dweights must be contiguous float32 of {tokens * slots} elements")
-    _done(_b.load().mxfp8_expert_weight_grad(_b._ptr(dy), _b._dtype_code(dy.dtype), ld_dy, _b._ptr(c), _b._dtype_code(c.dtype), rows, cols, ldc,
+    _check_status(_b.load().mxfp8_expert_weight_grad(_b._ptr(dy), _b._dtype_code(dy.dtype), ld_dy, _b._ptr(c), _b._dtype_code(c.dtype), rows, cols, ldc,
                                              _b._ptr(positions), tokens, slots, _b._ptr(dweights), _b._stream(stream)), "mxfp8_expert_weight_grad")
 
 
@@ -150,6 +163,8 @@ def _activations(x):
 
 def mxfp8_fp4_gemv_ex(x, w_q, w_s, c, scale_layout=SCALES_ROWMAJOR, stream=None) -> None:
     """c [M x N] (float32/bfloat16) = x [M x K] bfloat16 times MXFP4 weights w_q [N x K/2], w_s transposed: for a few rows."""
+    if _fast("fp4_gemv", "mxfp8_fp4_gemv_ex", x, w_q, w_s, c, scale_layout, stream):
+        return
     _ready(x, w_q, w_s, c)
     ldx = _activations(x)
     (M, K), N = x.shape, c.shape[1] if c.dim() == 2 else -1
@@ -157,13 +172,15 @@ def mxfp8_fp4_gemv_ex(x, w_q, w_s, c, scale_layout=SCALES_ROWMAJOR, stream=None)
         raise ValueError(f"w_q must be dense uint8 [{N} x {K // 2}], K a multiple of 32")
     _b._check_scales(w_s, N, K, scale_layout, "w_s")
     ldc = _matrix(c, "c", M, N)
-    _done(_b.load().mxfp8_fp4_gemv_ex(_b._ptr(x), ldx, _b._ptr(w_q), _b._ptr(w_s), M, N, K, _b._ptr(c), _b._dtype_code(c.dtype), ldc, scale_layout,
+    _check_status(_b.load().mxfp8_fp4_gemv_ex(_b._ptr(x), ldx, _b._ptr(w_q), _b._ptr(w_s), M, N, K, _b._ptr(c), _b._dtype_code(c.dtype), ldc, scale_layout,
                                       _b._stream(stream)), "mxfp8_fp4_gemv_ex")
 
 
 def mxfp8_fp4_gemv_grouped_ex(x, sources, slots, w_q, w_s, group_ends, c, scale_layout=SCALES_ROWMAJOR, stream=None) -> None:
     """Row r of c [M x N] = x[sources[r] // slots] (x[r] with sources None) times the weights of the expert that owns row r: w_q
     [groups x N x K/2], w_s (groups scale operands). Rows from the last end on are left as they were."""
+    if _fast("fp4_gemv_grouped", "mxfp8_fp4_gemv_grouped_ex", x, sources, slots, w_q, w_s, group_ends, c, scale_layout, stream):
+        return
     _ready(x, sources, w_q, w_s, group_ends, c)
     ldx = _activations(x)
     tokens, K = x.shape
@@ -181,7 +198,7 @@ def mxfp8_fp4_gemv_grouped_ex(x, sources, slots, w_q, w_s, group_ends, c, scale_
     if w_s.dtype != torch.uint8 or not w_s.is_contiguous() or w_s.numel() != groups * mxfp8_scale_bytes(N, K, scale_layout):
         raise ValueError("w_s must be dense uint8 with one scale operand per expert")
     ldc = _matrix(c, "c")
-    _done(_b.load().mxfp8_fp4_gemv_grouped_ex(_b._ptr(x), tokens, ldx, _b._ptr(sources), slots, _b._ptr(w_q), _b._ptr(w_s), _b._ptr(group_ends), groups,
+    _check_status(_b.load().mxfp8_fp4_gemv_grouped_ex(_b._ptr(x), tokens, ldx, _b._ptr(sources), slots, _b._ptr(w_q), _b._ptr(w_s), _b._ptr(group_ends), groups,
                                               M, N, K, _b._ptr(c), _b._dtype_code(c.dtype), ldc, scale_layout, _b._stream(stream)),
           "mxfp8_fp4_gemv_grouped_ex")
 

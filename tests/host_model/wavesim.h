@@ -257,6 +257,23 @@ inline int shfl(int v, int src)
 }
 inline int shfl_xor(int v, int mask) { return shfl(v, g.cur->lane ^ mask); }
 
+// v_permlane{32,16}_swap_b32: the upper half of the lanes (the odd rows of 16) of the first register changes places with the lower half (the
+// even rows) of the second
+typedef unsigned int v2ui __attribute__((ext_vector_type(2)));
+inline v2ui permlane_swap(uint32_t a, uint32_t b, int distance)
+{
+    struct Pub {
+        uint32_t a, b;
+    } pub{a, b};
+    Wave &w = publish(pub);
+    const int lane = g.cur->lane, other = lane ^ distance;
+    if (!w.present[other])
+        fail("a lane swap reads lane %d, which is not active", other);
+    const Pub o = peek<Pub>(w, other);
+    unpublish();
+    return lane & distance ? v2ui{o.b, b} : v2ui{a, o.a};
+}
+
 inline uint64_t ballot(bool b)
 {
     Wave &w = publish((int)b);
@@ -271,14 +288,23 @@ inline uint64_t ballot(bool b)
 inline int update_dpp(int old, int src, int ctrl, int row_mask, int bank_mask, bool bound_ctrl)
 {
     (void)old;
-    (void)bound_ctrl;
     if (row_mask != 0xF || bank_mask != 0xF)
         fail("DPP row/bank masks other than 0xF are not modelled");
     const int lane = g.cur->lane;
     int from;
     if (ctrl >= 0 && ctrl <= 0xFF)
         from = (lane & ~3) | ((ctrl >> (2 * (lane & 3))) & 3);  // quad_perm
-    else if (ctrl == 0x140)
+    else if (ctrl > 0x110 && ctrl <= 0x11F) {  // row_shr; lanes before the row's first give 0 (bound_ctrl)
+        const int by = ctrl - 0x110;
+        if (!bound_ctrl)
+            fail("row_shr without bound_ctrl is not modelled");
+        Wave &w = publish(src);
+        const int r = (lane & 15) >= by ? peek<int>(w, lane - by) : 0;
+        if ((lane & 15) >= by && !w.present[lane - by])
+            fail("DPP reads lane %d, which is not active", lane - by);
+        unpublish();
+        return r;
+    } else if (ctrl == 0x140)
         from = (lane & ~15) | (15 - (lane & 15));  // row_mirror
     else if (ctrl == 0x141)
         from = (lane & ~7) | (7 - (lane & 7));  // row_half_mirror

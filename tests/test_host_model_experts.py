@@ -18,8 +18,10 @@ ORDERS = ["up", "down"]
 
 @pytest.fixture(scope="session")
 def driver():
-    res = subprocess.run([BUILD, "--experts", BINARY], capture_output=True, text=True)
+    mine = f"{BINARY}.{os.getpid()}"   # test processes side by side do not build over each other
+    res = subprocess.run([BUILD, "--experts", mine], capture_output=True, text=True)
     assert res.returncode == 0, res.stderr[-4000:]
+    os.replace(mine, BINARY)
     return BINARY
 
 
