@@ -150,8 +150,8 @@ struct NoRows {
 // src_s = its scale bytes in the same layout as the outputs. Every value is decoded exactly on load and then
 // treated like an FP32 source: this derives the column copy of a tensor from its row copy (single-copy
 // storage, Section 5) at the price of a second rounding.
-// Rows (default: none): the source's rows are not consecutive; rows->load(r, c) gives VEC elements of row r of the tile from column c of
-// the tensor on, in the register layout of BF16, and src and ld_bytes are not looked at.
+// Rows (default: none): the source's rows are not consecutive; source_rows->load(x, r, c, active) fills x, in the register layout of BF16,
+// with rows r .. r + ROWS - 1 of the tile from column c of the tensor on, zeros if not active, and src and ld_bytes are not looked at.
 // Tile (tile_y, tile_x) of the tensor by a workgroup of kQuantThreads work-items; the caller separates two tiles that use
 // the same LDS with a barrier.
 template <bool BF16, bool ROW, bool COL, bool TILED, int MODE, bool MXSRC = false, class Rows = NoRows>
@@ -205,16 +205,15 @@ __device__ __forceinline__ void quantize_tile(
         __syncthreads();
     }
     uint4 x[ROWS];
+    if constexpr (Rows::kGiven)
+        source_rows->load(x, lrow0, col0, active);
 #pragma unroll
-    for (int i = 0; i < ROWS; ++i) {
+    for (int i = 0; i < (Rows::kGiven ? 0 : ROWS); ++i) {
         x[i] = make_uint4(0, 0, 0, 0);
         if constexpr (MXSRC) {
             if (active)
                 x[i] = decode_mx4(*reinterpret_cast<const uint32_t *>(lds_src + (lrow0 + i) * kTile + lcol0),
                                   (lds_src_s[lrow0 + i] >> (8 * (lcol0 / kBlock))) & 0xFFu);
-        } else if constexpr (Rows::kGiven) {
-            if (active)
-                x[i] = source_rows->load(lrow0 + i, col0);
         } else if (active) {
             x[i] = stream_load(reinterpret_cast<const uint4 *>(src + (row0 + i) * ld_bytes + col0 * ESIZE));
         }

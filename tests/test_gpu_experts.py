@@ -166,6 +166,14 @@ def test_quantize_padded_source_rows_one_token_and_no_entry():
     _check_quantize(buf[:, :96], src32, _experts(rng, 40, 2, 4), 4, 32, 2, None, "both", False, extra_rows=200, whole=True)
 
 
+def test_quantize_of_no_tokens_writes_zeros():
+    out = {k: torch.full(s, 0xA5, dtype=torch.uint8, device="cuda") for k, s in (("q_row", (64, 96)), ("s_row", (64, 3)), ("q_colT", (96, 64)), ("s_colT", (96, 2)))}
+    for weights in (None, torch.empty((0, 2), device="cuda")):
+        mx.mxfp8_expert_quantize_ex(torch.empty((0, 96), device="cuda"), _dev(np.zeros(64, np.int32)), None, 2, weights, "both", **out)
+        torch.cuda.synchronize()
+        assert all((v.cpu() == 0).all() for v in out.values())
+
+
 def test_quantize_takes_bad_plans_without_leaving_its_buffers():
     rng = np.random.default_rng(4)
     src, src32 = _values(rng, 10, 64, False)
