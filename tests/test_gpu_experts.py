@@ -92,7 +92,7 @@ def test_sort_without_experts_and_of_wide_numbers():
 
 
 @pytest.mark.parametrize("index64", [False, True], ids=["i32", "i64"])
-@pytest.mark.parametrize("entries,groups,align", [(32768, 256, 128), (32769, 96, 64), (131072, 128, 128), (40000, 4096, 1), (70001, 1, 32), (524288, 256, 128)])
+@pytest.mark.parametrize("entries,groups,align", [(8192, 64, 1), (8193, 64, 128), (8200, 4096, 2), (300, 256, 128), (32768, 256, 128), (32769, 96, 64), (131072, 128, 128), (40000, 4096, 1), (70001, 1, 32), (524288, 256, 128)])
 def test_sort_full_size(entries, groups, align, index64):
     _check_sort(_experts(np.random.default_rng(entries), entries, 1, groups), groups, align, 11, index64)
 

@@ -85,7 +85,7 @@ def test_sort_in_two_launches(driver, tmp_path, groups):
     experts = np.random.default_rng(1).integers(-1, groups, entries)
     rows = ref.rows_needed(entries, groups, align) + 3
     out = (Case(tmp_path, "sort").given(experts.astype(np.int32)).number(0, entries, groups, align, rows).output("positions", 4 * entries)
-           .output("sources", 4 * rows).output("ends", 4 * groups).output("workspace", -(-entries // 4096) * groups * 4).run(driver))
+           .output("sources", 4 * rows).output("ends", 4 * groups).output("workspace", -(-entries // 1024) * groups * 4).run(driver))
     for name, want in zip(("positions", "sources", "ends"), ref.plan(experts, groups, align, rows)):
         assert np.array_equal(_i32(out[name]), want), name
 
