@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
         MXFP8_PIN();
     };
     // Places are XORed so that the sixteen lanes that are served together hit different banks.
-    auto multiply_units = [&](const Units &d, int count) __attribute__((always_inline)) {
+    auto stage = [&](const Units &d) __attribute__((always_inline)) {
         MXFP8_FENCE();
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -157,6 +157,8 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
         lds_s[s_row * 4 + s_unit] = d.s;
         __builtin_amdgcn_wave_barrier();
         MXFP8_FENCE();
+    };
+    auto multiply = [&](int count) __attribute__((always_inline)) {
         const uint4 scales = *reinterpret_cast<const uint4 *>(lds_s + r * 4);
         const uint32_t s[4] = {scales.x, scales.y, scales.z, scales.w};
 #pragma unroll
@@ -179,10 +181,16 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
         }
         MXFP8_PIN();
     };
-    for (int u = begin; u < end; u += U) {
+    // The next units are on their way while those in LDS are multiplied.
+    if (begin < end) {
         Units d;
-        load(d, u);
-        multiply_units(d, end - u);
+        load(d, begin);
+        for (int u = begin; u < end; u += U) {
+            stage(d);
+            if (u + U < end)
+                load(d, u + U);
+            multiply(end - u);
+        }
     }
     if (any && nb % kUnit && wk == WK - 1) {  // one to three blocks behind the whole units
         const int rest = nb % kUnit;
@@ -196,7 +204,8 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
 #pragma unroll
             for (int q = 0; q < XL; ++q)
                 d.x[q] = *reinterpret_cast<const uint4 *>(xp[q] + (int64_t)units * 256);
-        multiply_units(d, 1);
+        stage(d);
+        multiply(1);
     }
 
     // ---- sums of the wavefronts along K, in their order; wavefront k of them then stores the tiles k, k + WK, ...
