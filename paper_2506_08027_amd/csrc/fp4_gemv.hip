@@ -1,6 +1,6 @@
 // Products of a few rows of BF16 activations with MXFP4 weights (include/mxfp8_experts.h): C[m, n] = sum_k x[m, k] W[n, k].
 //
-// Every weight is read once for up to 64 rows of x, so HBM is the bound as long as all else hides behind it. A wavefront takes 16 rows of
+// Every weight is read once for up to 32 rows of x, so HBM is the bound as long as all else hides behind it. A wavefront takes 16 rows of
 // W and a contiguous part of K, in units of 128 k: the 4-bit codes are widened to BF16, scale included, by
 // v_cvt_scalef32_pk_bf16_fp4 (exact where BF16 holds the value) and multiplied on v_mfma_f32_16x16x32_bf16, W as its first operand. Where a
 // workgroup's wavefronts share rows of W, their sums are joined in LDS in a fixed order; until then no wavefront waits for another.
@@ -67,8 +67,9 @@ template <int R> __device__ __forceinline__ GemvPiece grouped_piece(const int32_
     return {0, 0, 0};
 }
 
-// XR rows of x (up to 16, or a multiple of it); WK wavefronts along K, the others along N. U units (4, 2 or 1) are loaded at a time.
-template <int XR, int WK, int U, bool TILED, bool GROUPED>
+// XR rows of x (up to 16, or a multiple of it); NT tiles of 16 rows of W a wavefront; WK wavefronts along K, the others along N. U units (4,
+// 2 or 1) are loaded at a time.
+template <int XR, int NT, int WK, int U, bool TILED, bool GROUPED>
 __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *__restrict__ x, int64_t ldx_bytes, GemvRows map,
                                                                 const uint8_t *__restrict__ w_q, const uint8_t *__restrict__ w_s, int M, int N, int nb,
                                                                 uint32_t blocks_n, uint8_t *__restrict__ c, bool c_bf16, int64_t ldc, bool c_vector)
@@ -76,9 +77,9 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
     constexpr int R = XR, MT = (XR + 15) / 16, WN = kGemvWaves / WK;
     constexpr int LANES = 16 * U;             // lanes of a row of x in a load
     constexpr int XL = XR * LANES > 64 ? XR * LANES / 64 : 1;  // loads of x
-    // LDS of a wavefront, in pieces of 16 bytes: x [row][unit][16], W [unit][row][4], scales [row] (the dwords of four units)
-    constexpr int XP = XR * LANES > 64 ? XR * LANES : 64, WP = U * 64;
-    __shared__ uint4 staged[kGemvWaves][XP + WP + 16];
+    // LDS of a wavefront, in pieces of 16 bytes: x [row][unit][16], W [tile][unit][row][4], scales [tile][row] (the dwords of four units)
+    constexpr int XP = XR * LANES > 64 ? XR * LANES : 64, WP = NT * U * 64;
+    __shared__ uint4 staged[kGemvWaves][XP + WP + NT * 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int wk = wave % WK, wn = wave / WK;
     const uint32_t block = blockIdx.x % blocks_n, u_piece = blockIdx.x / blocks_n;
@@ -115,26 +116,33 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
         xp[q] = x + (row < 0 ? first_row : row) * ldx_bytes + lane_piece * 16;
     }
     // ---- rows of W: four lanes a row, from block 4u + lane % 4 on; scales of the next four units, one dword a lane
-    const int n0 = ((int)block * WN + wn) * 16;
-    const int w_row = min(n0 + (lane >> 2), N - 1), s_unit = TILED ? g : lane & 3, s_row = TILED ? r : lane >> 2, s_n = min(n0 + s_row, N - 1);
-    const uint8_t *const wq = w_q + p.expert * (GROUPED ? map.wq_group_bytes : 0) + w_row * ((int64_t)nb * 16) + (lane & 3) * 16;
-    const uint8_t *const ws = w_s + p.expert * (GROUPED ? map.ws_group_bytes : 0) +
-                              (TILED ? ((int64_t)(s_n >> 6) * ((nb + 3) / 4) * 64 + (s_n & 63)) * 4 : (int64_t)s_n * nb);
+    const int n0 = ((int)block * WN + wn) * NT * 16;
+    const int s_unit = TILED ? g : lane & 3, s_row = TILED ? r : lane >> 2;
+    const uint8_t *wq[NT], *ws[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int w_row = min(n0 + t * 16 + (lane >> 2), N - 1), s_n = min(n0 + t * 16 + s_row, N - 1);
+        wq[t] = w_q + p.expert * (GROUPED ? map.wq_group_bytes : 0) + w_row * ((int64_t)nb * 16) + (lane & 3) * 16;
+        ws[t] = w_s + p.expert * (GROUPED ? map.ws_group_bytes : 0) + (TILED ? ((int64_t)(s_n >> 6) * ((nb + 3) / 4) * 64 + (s_n & 63)) * 4 : (int64_t)s_n * nb);
+    }
 
     struct Units {
-        uint4 w[U], x[XL];
-        uint32_t s;
+        uint4 w[NT][U], x[XL];
+        uint32_t s[NT];
     };
     uint4 *const lds_x = staged[wave], *const lds_w = lds_x + XP;
     uint32_t *const lds_s = reinterpret_cast<uint32_t *>(lds_w + WP);
-    v4f acc[MT] = {};
+    v4f acc[NT][MT] = {};
     const int units = any ? nb / kUnit : 0;  // whole ones
     const int begin = (int)((int64_t)units * wk / WK), end = (int)((int64_t)units * (wk + 1) / WK);
     auto load = [&](Units &d, int u) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < U; ++j)
-            d.w[j] = stream_load(reinterpret_cast<const uint4 *>(wq + (int64_t)min(u + j, end - 1) * 64));
-        __builtin_memcpy(&d.s, ws + (int64_t)min(u + s_unit, end - 1) * (TILED ? 256 : 4), 4);
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int j = 0; j < U; ++j)
+                d.w[t][j] = stream_load(reinterpret_cast<const uint4 *>(wq[t] + (int64_t)min(u + j, end - 1) * 64));
+            __builtin_memcpy(&d.s[t], ws[t] + (int64_t)min(u + s_unit, end - 1) * (TILED ? 256 : 4), 4);
+        }
         const int last = (end - u) * 16 - 1;  // pieces of x behind the last unit are not multiplied: any others will do
 #pragma unroll
         for (int q = 0; q < XL; ++q)
@@ -152,32 +160,44 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
                 lds_x[m * LANES + (lane_piece ^ (m & 15))] = d.x[q];
         }
 #pragma unroll
-        for (int j = 0; j < U; ++j)
-            lds_w[j * 64 + (lane & ~3) + ((lane ^ (lane >> 4)) & 3)] = d.w[j];
-        lds_s[s_row * 4 + s_unit] = d.s;
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int j = 0; j < U; ++j)
+                lds_w[(t * U + j) * 64 + (lane & ~3) + ((lane ^ (lane >> 4)) & 3)] = d.w[t][j];
+            lds_s[t * 64 + s_row * 4 + s_unit] = d.s[t];
+        }
         __builtin_amdgcn_wave_barrier();
         MXFP8_FENCE();
     };
     auto multiply = [&](int count) __attribute__((always_inline)) {
-        const uint4 scales = *reinterpret_cast<const uint4 *>(lds_s + r * 4);
-        const uint32_t s[4] = {scales.x, scales.y, scales.z, scales.w};
+        uint32_t s[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const uint4 scales = *reinterpret_cast<const uint4 *>(lds_s + t * 64 + r * 4);
+            s[t][0] = scales.x, s[t][1] = scales.y, s[t][2] = scales.z, s[t][3] = scales.w;
+        }
 #pragma unroll
         for (int j = 0; j < U; ++j) {
             if (j >= count)
                 break;
-            const uint4 w4 = lds_w[j * 64 + r * 4 + (g ^ (r >> 2))];
-            const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-            const float scale = scale_operand((s[j] >> (8 * g)) & 0xFFu);
+            v8bf a[NT][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const v8bf a = fp4_word_bf16(w[i], scale);
+            for (int t = 0; t < NT; ++t) {
+                const uint4 w = lds_w[(t * U + j) * 64 + r * 4 + (g ^ (r >> 2))];
+                const float scale = scale_operand((s[t][j] >> (8 * g)) & 0xFFu);
+                a[t][0] = fp4_word_bf16(w.x, scale), a[t][1] = fp4_word_bf16(w.y, scale);
+                a[t][2] = fp4_word_bf16(w.z, scale), a[t][3] = fp4_word_bf16(w.w, scale);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int t = 0; t < MT; ++t) {
                     const int m = min(t * 16 + r, XR - 1);
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(v8bf, lds_x[m * LANES + ((j * 16 + 4 * g + i) ^ (m & 15))]), acc[t],
-                                                                     0, 0, 0);
+                    const v8bf b = __builtin_bit_cast(v8bf, lds_x[m * LANES + ((j * 16 + 4 * g + i) ^ (m & 15))]);
+#pragma unroll
+                    for (int k = 0; k < NT; ++k)
+                        acc[k][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[k][i], b, acc[k][t], 0, 0, 0);
                 }
-            }
         }
         MXFP8_PIN();
     };
@@ -195,11 +215,14 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
     if (any && nb % kUnit && wk == WK - 1) {  // one to three blocks behind the whole units
         const int rest = nb % kUnit;
         Units d = {};
-        if ((lane & 3) < rest)
-            d.w[0] = *reinterpret_cast<const uint4 *>(wq + (int64_t)units * 64);
-        if (s_unit == 0)
-            for (int b = 0; b < rest; ++b)
-                d.s |= (uint32_t)ws[(int64_t)units * (TILED ? 256 : 4) + b] << (8 * b);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            if ((lane & 3) < rest)
+                d.w[t][0] = *reinterpret_cast<const uint4 *>(wq[t] + (int64_t)units * 64);
+            if (s_unit == 0)
+                for (int b = 0; b < rest; ++b)
+                    d.s[t] |= (uint32_t)ws[t][(int64_t)units * (TILED ? 256 : 4) + b] << (8 * b);
+        }
         if (lane_piece < rest * 4)
 #pragma unroll
             for (int q = 0; q < XL; ++q)
@@ -208,30 +231,31 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
         multiply(1);
     }
 
-    // ---- sums of the wavefronts along K, in their order; wavefront k of them then stores the tiles k, k + WK, ...
+    // ---- sums of the wavefronts along K, in their order; wavefront k of them then stores the tiles k, k + WK, ... of NT x MT
     if constexpr (WK > 1) {
-        static_assert(MT * 64 <= XP + WP, "the sums take the place of what is staged");
+        static_assert(NT * MT * 64 <= XP + WP, "the sums take the place of what is staged");
         MXFP8_FENCE();
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-            reinterpret_cast<v4f *>(staged[wave])[t * 64 + lane] = acc[t];
+        for (int k = 0; k < NT * MT; ++k)
+            reinterpret_cast<v4f *>(staged[wave])[k * 64 + lane] = acc[k / MT][k % MT];
         __syncthreads();
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-            if (t % WK == wk) {
-                acc[t] = reinterpret_cast<const v4f *>(staged[wn * WK])[t * 64 + lane];
+        for (int k = 0; k < NT * MT; ++k)
+            if (k % WK == wk) {
+                v4f sum = reinterpret_cast<const v4f *>(staged[wn * WK])[k * 64 + lane];
 #pragma unroll
-                for (int k = 1; k < WK; ++k)
-                    acc[t] += reinterpret_cast<const v4f *>(staged[wn * WK + k])[t * 64 + lane];
+                for (int w = 1; w < WK; ++w)
+                    sum += reinterpret_cast<const v4f *>(staged[wn * WK + w])[k * 64 + lane];
+                acc[k / MT][k % MT] = sum;
             }
     }
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int m = t * 16 + r, n = n0 + 4 * g;
-        if ((WK > 1 && t % WK != wk) || m >= p.count || n >= N)
+    for (int k = 0; k < NT * MT; ++k) {
+        const int m = k % MT * 16 + r, n = n0 + k / MT * 16 + 4 * g;
+        if ((WK > 1 && k % WK != wk) || m >= p.count || n >= N)
             continue;
-        const v4f sum = GROUPED && at[t] < 0 ? v4f{0, 0, 0, 0} : acc[t];
+        const v4f sum = GROUPED && at[k % MT] < 0 ? v4f{0, 0, 0, 0} : acc[k / MT][k % MT];
         uint8_t *const to = c + ((p.first + m) * ldc + n) * (c_bf16 ? 2 : 4);
         if (c_bf16) {
             const v2bf a = {(__bf16)sum[0], (__bf16)sum[1]}, b = {(__bf16)sum[2], (__bf16)sum[3]};
@@ -260,35 +284,38 @@ static int64_t gemv_pieces(const GemvRows &map, int64_t M, int R)
     return map.ends ? some + (M - some) / R : (M + R - 1) / R;
 }
 
-template <int XR, int WK, int U, bool TILED>
+template <int XR, int NT, int WK, int U, bool TILED>
 static hipError_t launch_fp4_gemv_t(const void *x, int64_t ldx, const GemvRows &map, const uint8_t *w_q, const uint8_t *w_s, int64_t M, int64_t N,
                                     int64_t K, void *c, bool c_bf16, int64_t ldc, hipStream_t stream)
 {
-    constexpr int COLS = kGemvWaves / WK * 16;  // rows of W of a workgroup
+    constexpr int COLS = kGemvWaves / WK * NT * 16;  // rows of W of a workgroup
     const int64_t pieces = gemv_pieces(map, M, XR);
     const int64_t blocks_n = (N + COLS - 1) / COLS;
     if (blocks_n * pieces > 0x7FFFFFFF)
         return hipErrorInvalidConfiguration;
     const bool vector = reinterpret_cast<uintptr_t>(c) % 16 == 0 && (ldc * (c_bf16 ? 2 : 4)) % 16 == 0;
-    auto kern = map.ends ? fp4_gemv_kernel<XR, WK, U, TILED, true> : fp4_gemv_kernel<XR, WK, U, TILED, false>;
+    auto kern = map.ends ? fp4_gemv_kernel<XR, NT, WK, U, TILED, true> : fp4_gemv_kernel<XR, NT, WK, U, TILED, false>;
     hipLaunchKernelGGL(kern, dim3((unsigned)(blocks_n * pieces)), dim3(kGemvThreads), 0, stream, static_cast<const uint8_t *>(x), ldx * 2, map, w_q, w_s,
                        (int)M, (int)N, (int)(K / kBlock), (uint32_t)blocks_n, static_cast<uint8_t *>(c), c_bf16, ldc, vector);
     return hipGetLastError();
 }
 
-template <int XR, int U, bool TILED>
+template <int XR, int NT, int U, bool TILED>
 static hipError_t launch_fp4_gemv_rows(const void *x, int64_t ldx, const GemvRows &map, const uint8_t *w_q, const uint8_t *w_s, int64_t M, int64_t N,
                                        int64_t K, void *c, bool c_bf16, int64_t ldc, hipStream_t stream)
 {
-    // As many wavefronts along K as have four units each, up to some 8192 in all.
-    const int64_t tiles = (N + 15) / 16 * gemv_pieces(map, M, XR), units = K / (kUnit * kBlock);
+    // As many wavefronts along K as have four units each, up to what the LDS lets be resident: 2048 with 16 rows of x and more, else some
+    // 8192. In us with 1 | 2 | 4 | 8 along K: [1 x 4096 x 14336] 40.7 | 22.5 | 13.8 | 10.7, [1 x 28672 x 4096] 14.4 | 16.7 | 15.8 | 16.4,
+    // [64 x 28672 x 4096] 71.4 | 43.8 | 50.7 | 55.1, 48 tokens x 4 of 64 experts [5632 x 2048] 78.7 | 75.1 | 83.6 | 107.7.
+    const int64_t tiles = (N + 16 * NT - 1) / (16 * NT) * gemv_pieces(map, M, XR), units = K / (kUnit * kBlock);
+    const int64_t most = XR >= 16 ? 2048 : 8192;
     int wk = 1;
-    while (wk < kGemvWaves && units >= 8 * wk && tiles * wk * 2 <= 8192)
+    while (wk < kGemvWaves && units >= 8 * wk && (tiles * wk * 2 <= most || (NT > 1 && wk == 1)))
         wk *= 2;
-    auto launch = wk == 1   ? launch_fp4_gemv_t<XR, 1, U, TILED>
-                  : wk == 2 ? launch_fp4_gemv_t<XR, 2, U, TILED>
-                  : wk == 4 ? launch_fp4_gemv_t<XR, 4, U, TILED>
-                            : launch_fp4_gemv_t<XR, 8, U, TILED>;
+    auto launch = wk == 1   ? launch_fp4_gemv_t<XR, NT, 1, U, TILED>
+                  : wk == 2 ? launch_fp4_gemv_t<XR, NT, 2, U, TILED>
+                  : wk == 4 ? launch_fp4_gemv_t<XR, NT, 4, U, TILED>
+                            : launch_fp4_gemv_t<XR, NT, 8, U, TILED>;
     return launch(x, ldx, map, w_q, w_s, M, N, K, c, c_bf16, ldc, stream);
 }
 
@@ -301,12 +328,18 @@ hipError_t launch_fp4_gemv(const void *x, int64_t tokens, int64_t ldx, const int
     const int64_t rows = !group_ends ? M : M == 1 || (sources && tokens == 1) ? 1 : (M + groups - 1) / groups * 3 / 2 + 1;
     auto launch = [&](auto tiled) {
         constexpr bool T = decltype(tiled)::value;
-        auto pick = rows <= 1    ? launch_fp4_gemv_rows<1, 4, T>
-                    : rows <= 4  ? launch_fp4_gemv_rows<4, 4, T>
-                    : rows <= 8  ? launch_fp4_gemv_rows<8, 2, T>
-                    : rows <= 16 ? launch_fp4_gemv_rows<16, 2, T>
-                    : rows <= 32 ? launch_fp4_gemv_rows<32, 1, T>
-                                 : launch_fp4_gemv_rows<64, 1, T>;
+        // Two or four tiles of W a wavefront, so that x is fetched and reordered for more of them, where there are tiles enough (of 16
+        // rows of W and the XR rows of a piece). In us, one tile | two | four: [8 x 28672 x 4096] 22.2 | 19.2, [64 x 28672 x 4096]
+        // 73.2 | 50.9 | 43.8, [64 x 4096 x 4096] 12.2 | 10.2 | 13.7, [32 x 4096 x 4096] 7.9 | 9.6 | 12.5, [8 x 4096 x 4096] 5.2 | 6.2.
+        const int64_t n16 = (N + 15) / 16;
+        auto tiles = [&](int xr) { return n16 * gemv_pieces(map, M, xr); };
+        auto pick = rows <= 1    ? launch_fp4_gemv_rows<1, 1, 4, T>
+                    : rows <= 4  ? launch_fp4_gemv_rows<4, 1, 4, T>
+                    : rows <= 8  ? (tiles(8) < 1024 ? launch_fp4_gemv_rows<8, 1, 2, T> : launch_fp4_gemv_rows<8, 2, 2, T>)
+                    : rows <= 16 ? (tiles(16) < 1024 ? launch_fp4_gemv_rows<16, 1, 2, T> : launch_fp4_gemv_rows<16, 2, 2, T>)
+                    : tiles(32) < 512  ? launch_fp4_gemv_rows<32, 1, 1, T>
+                    : tiles(32) < 2048 ? launch_fp4_gemv_rows<32, 2, 1, T>
+                                       : launch_fp4_gemv_rows<32, 4, 1, T>;
         return pick(x, ldx, map, w_q, w_s, M, N, K, c, c_bf16, ldc, stream);
     };
     return tiled_scales ? launch(std::true_type{}) : launch(std::false_type{});

@@ -136,7 +136,8 @@ def test_gemv_of_nothing():
                        torch.zeros((3, 2), dtype=torch.uint8, device="cuda")).shape == (0, 3)
 
 
-@pytest.mark.parametrize("M,N,K,tiled", [(1, 6144, 4096, False), (12, 4096, 14336, True), (3, 5001, 14304, False), (48, 2048, 4096, True), (16, 4096, 4096, False)])
+@pytest.mark.parametrize("M,N,K,tiled", [(8, 16400, 160, False), (7, 16384, 2080, True), (16, 16400, 96, True), (13, 17000, 1056, False), (32, 33000, 160, False),
+                                         (64, 20000, 640, True), (40, 4100, 544, False), (200, 3000, 320, True), (1, 6144, 4096, False), (12, 4096, 14336, True), (3, 5001, 14304, False), (48, 2048, 4096, True), (16, 4096, 4096, False)])
 def test_gemv_full_size(M, N, K, tiled):
     rng = np.random.default_rng(N)
     x, x32 = _x(rng, M, K)
@@ -206,7 +207,8 @@ def test_grouped_gemv_takes_bad_plans_without_leaving_its_buffers():
         assert np.array_equal(np.isnan(_host(c)), ~owned) and (np.abs(_host(c) - want)[owned] <= _bound(want, mag, 64, False)[owned]).all()
 
 
-@pytest.mark.parametrize("tokens,slots,groups,N,K,tiled", [(1, 8, 64, 704, 2048, False), (48, 4, 32, 512, 1024, True), (200, 8, 16, 256, 512, False)])
+@pytest.mark.parametrize("tokens,slots,groups,N,K,tiled", [(1, 8, 64, 704, 2048, False), (48, 4, 32, 512, 1024, True), (200, 8, 16, 256, 512, False),
+                                                             (60, 4, 32, 1040, 288, True), (300, 8, 32, 1000, 96, False), (20, 2, 3, 24, 4096, False)])
 def test_grouped_gemv_full_size(tokens, slots, groups, N, K, tiled):
     rng = np.random.default_rng(tokens)
     experts = np.stack([rng.permutation(groups)[:slots] for _ in range(tokens)])

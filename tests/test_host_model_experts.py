@@ -167,6 +167,18 @@ def _gemv_values(rng, rows, K, ldx):
 @pytest.mark.parametrize("tiled,bf16,off", [(False, False, 0), (True, True, 0), (False, True, 2)])
 @pytest.mark.parametrize("M,N,K,ldx,ldc", [(1, 1, 32, 32, 1), (3, 21, 160, 168, 24), (16, 16, 1056, 1056, 16), (17, 33, 96, 104, 40), (50, 18, 64, 64, 18), (70, 16, 288, 288, 19)])
 def test_gemv(driver, tmp_path, M, N, K, ldx, ldc, tiled, bf16, off, order):
+    _check_gemv(driver, tmp_path, M, N, K, ldx, ldc, tiled, bf16, off, order)
+
+
+# tiles of W by twos and fours: many columns
+@pytest.mark.parametrize("M,N,K,tiled", [(6, 16390, 32, True), (11, 16384, 64, False), (20, 8200, 32, False),
+                                         pytest.param(40, 16390, 32, True, marks=pytest.mark.slow),
+                                         pytest.param(8, 16390, 1120, False, marks=pytest.mark.slow), (33, 4100, 160, True)])
+def test_gemv_of_many_columns(driver, tmp_path, M, N, K, tiled):
+    _check_gemv(driver, tmp_path, M, N, K, K, N, tiled, False, 0, "down")
+
+
+def _check_gemv(driver, tmp_path, M, N, K, ldx, ldc, tiled, bf16, off, order):
     rng = np.random.default_rng(K)
     flat, x = _gemv_values(rng, M, K, ldx)
     w_q, w_s = rng.integers(0, 256, (N, K // 2), dtype=np.uint8), rng.integers(126, 129, (N, K // 32)).astype(np.uint8)
