@@ -51,10 +51,11 @@ mxfp8_status mxfp8_expert_sort(const void *experts, mxfp8_index experts_type, in
                                void *hip_stream);
 
 /*
- * MXFP8 copies of sorted rows: mxfp8_quantize_ex of the FP32 tensor v [rows x cols]
+ * MXFP8 copies of sorted rows: what mxfp8_quantize_ex makes of the tensor v [rows x cols]
  *   v[r, :] = weights[i] * src[i / slots, :] with i = sources[r]  (without weights: src[i / slots, :])
  *   v[r, :] = 0 where sources[r] is -1
- * which is never stored. The product with the weight is rounded once, to FP32. src [tokens x cols] FP32 or BF16, leading dimension
+ * which is never stored. The product with the weight is rounded once, by the conversion (a product below 2^-102 may have been
+ * rounded to FP32 before; one beyond FP32 counts as infinite). src [tokens x cols] FP32 or BF16, leading dimension
  * ld_src; weights [tokens x slots] FP32, NULL for none; group_ends [groups] as mxfp8_expert_sort gave them: rows behind the last
  * 128-row tile that holds a row of an expert are left as they were (NULL with groups == 0: all rows are converted). An entry number
  * outside [-1, tokens * slots) counts as -1 and an end outside [0, rows] as the nearer of the two, so that no access leaves a buffer.

@@ -27,6 +27,18 @@ def rows_needed(entries, groups, align):
     return (entries + min(entries, groups) * (align - 1)) // align * align
 
 
+def product(w, x):
+    """w * x of float32 values as FP32 that stands for the exact product in a later rounding: where it is inexact, the neighbour with an
+    odd last bit (the product of two float32 is exact in float64). What the nearest value leaves is itself taken in FP32."""
+    with np.errstate(over="ignore", invalid="ignore", under="ignore"):
+        whole = w.astype(np.float64) * x.astype(np.float64)
+        p = (w * x).astype(np.float32)
+        rest = (whole - p.astype(np.float64)).astype(np.float32)
+    bits = p.view(np.int32)
+    move = np.isfinite(p) & (rest != 0) & (bits & 1 == 0)
+    return np.where(move, bits + np.where(np.signbit(rest) == np.signbit(p), 1, -1), bits).astype(np.int32).view(np.float32)
+
+
 def sorted_rows(src, sources, slots, weights=None):
     """FP32 rows as they are quantized; src float32."""
     v = np.zeros((sources.size, src.shape[1]), np.float32)
@@ -34,8 +46,7 @@ def sorted_rows(src, sources, slots, weights=None):
     at = sources[given]
     v[given] = src[at // slots]
     if weights is not None:
-        with np.errstate(over="ignore", invalid="ignore"):
-            v[given] *= weights.ravel()[at][:, None]
+        v[given] = product(np.broadcast_to(weights.ravel()[at][:, None], v[given].shape), v[given])
     return v
 
 

@@ -166,6 +166,33 @@ def test_quantize_padded_source_rows_one_token_and_no_entry():
     _check_quantize(buf[:, :96], src32, _experts(rng, 40, 2, 4), 4, 32, 2, None, "both", False, extra_rows=200, whole=True)
 
 
+def test_quantize_rounds_the_exact_product_once():
+    """Products next to a border of the conversion, where FP32's nearest value lies on the other side or on the border itself: the
+    result is that of the exact product (taken apart here in whole numbers)."""
+    rng = np.random.default_rng(17)
+    cols, n = 64, 4096
+    near = (1 + (2 * rng.integers(0, 8, n) + 1) / 16) * 2.0 ** rng.integers(-3, 4, n)     # midway between two E4M3 values
+    w = (1 + rng.random(n)).astype(np.float32)
+    x = np.nextafter((near / w).astype(np.float32), np.float32(100) * rng.choice([-1, 1], n).astype(np.float32))
+    src = np.zeros((n, cols), np.float32)
+    src[:, 0], src[:, 32] = x, x
+    src[:, 1] = np.float32(400) / w                                                        # a block maximum of about 400: scale 1
+    src[:, 33] = x * 0.5
+    q, s = (torch.empty((n, c), dtype=torch.uint8, device="cuda") for c in (cols, 2))
+    mx.mxfp8_expert_quantize_ex(_dev(src), _dev(np.arange(n, dtype=np.int32)), None, 1, _dev(w[:, None]), "rowwise", q, s)
+    torch.cuda.synchronize()
+    exact = src.astype(np.float64) * w.astype(np.float64)[:, None]                         # 48 bits: exact
+    scale = np.repeat(np.exp2(s.cpu().numpy().astype(np.float64) - 127), 32, 1)
+    assert (s.cpu().numpy()[:, 0] == 127).all()
+    t = exact / scale
+    step = np.exp2(np.floor(np.log2(np.maximum(np.abs(t), 2.0 ** -6))) - 3)
+    want = np.round(t / step) * step                                                       # ties to even; all of it exact in float64
+    got = oracle.dequantize(q.cpu().numpy(), s.cpu().numpy(), "f64") / scale
+    assert np.array_equal(got, want)
+    twice = (src * w[:, None]).astype(np.float64) / scale
+    assert (np.round(twice / step) * step != want).sum() > 0, "the inputs do not reach a border"
+
+
 def test_quantize_of_no_tokens_writes_zeros():
     out = {k: torch.full(s, 0xA5, dtype=torch.uint8, device="cuda") for k, s in (("q_row", (64, 96)), ("s_row", (64, 3)), ("q_colT", (96, 64)), ("s_colT", (96, 2)))}
     for weights in (None, torch.empty((0, 2), device="cuda")):
