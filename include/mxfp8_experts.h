@@ -72,8 +72,9 @@ mxfp8_status mxfp8_expert_quantize_ex(const void *src, mxfp8_dtype src_dtype, in
  * Sorted rows back to their tokens: out[t, :] = sum over j of weights[t, j] * c[positions[t, j], :] (without weights: the plain
  * sum, which is the gradient of the sorted copies), summed in FP32 in the order of j and rounded once. A position outside
  * [0, rows) adds nothing, whatever its weight; a token without any gets zeros. c [rows x cols] and out [tokens x cols] FP32 or
- * BF16, leading dimensions ldc, ld_out; positions [tokens x slots]; weights [tokens x slots] FP32 or NULL. cols % 32 == 0; c and
- * out 16-byte aligned, their leading dimensions multiples of 16 bytes; positions and weights 4-byte aligned. Sizes as above.
+ * BF16, leading dimensions ldc, ld_out; positions [tokens x slots]; weights [tokens x slots] FP32 or NULL. Any cols; c and out aligned
+ * to their element size (faster: they and their rows 16-byte aligned); positions and weights 4-byte aligned. Sizes as above, and
+ * tokens * ceil(cols / 512) < 2^31.
  */
 mxfp8_status mxfp8_expert_combine(const void *c, mxfp8_dtype c_dtype, int64_t rows, int64_t cols, int64_t ldc,
                                   const int32_t *positions, const float *weights, int64_t tokens, int32_t slots, void *out,
@@ -93,7 +94,8 @@ mxfp8_status mxfp8_expert_weight_grad(const void *dy, mxfp8_dtype dy_dtype, int6
  * C [M x N] = x [M x K] * W [N x K]^T for a few rows of BF16 activations and MXFP4 weights as mxfp8_fp4_quantize_ex stores them
  * (w_q [N x K/2], w_s [N x K/32] in `scale_layout`): the weights are widened to BF16, as mxfp8_fp4_dequantize_ex gives them, on their
  * way to the matrix instructions and accumulated in FP32; activations are not quantized. c FP32 or BF16 (RNE), leading dimension
- * ldc >= N. Meant for up to some tens of rows, where reading the weights is all the work; any M is right. M, N <= 2^30, K <= 2^24,
+ * ldc >= N. Meant for up to some tens of rows, where reading the weights is all the work; any M is right. M, N <= 2^30, K <= 2^24, at most 2^23 - 1 workgroups (of 16
+ * rows of W and 32 of x or more, each expert's rows apart; else MXFP8_ERR_SHAPE),
  * K % 32 == 0 (K == 0 stores zeros); x 16-byte aligned and ldx a multiple of 8; w_q and tiled w_s 16-byte aligned; c aligned to its
  * element size (faster: c and its rows 16-byte aligned). A 0xFF scale makes its output column NaN.
  */

@@ -93,14 +93,13 @@ mxfp8_status mxfp8_expert_combine(const void *c, mxfp8_dtype c_dtype, int64_t ro
 {
     if (!valid_dtype(c_dtype) || !valid_dtype(out_dtype))
         return MXFP8_ERR_DTYPE;
-    if (!valid_entries(tokens, slots) || rows < 0 || rows > kMaxRows || cols < 0 || cols > kMaxCols || cols % 32 || ldc < cols || ld_out < cols)
+    if (!valid_entries(tokens, slots) || rows < 0 || rows > kMaxRows || cols < 0 || cols > kMaxCols || ldc < cols || ld_out < cols)
         return MXFP8_ERR_SHAPE;
     if (tokens == 0 || cols == 0)
         return MXFP8_OK;
     if ((rows > 0 && !c) || !positions || !out)
         return MXFP8_ERR_NULL;
-    if (!aligned(c, 16) || !aligned(out, 16) || (ldc * esize(c_dtype)) % 16 || (ld_out * esize(out_dtype)) % 16 || !aligned(positions, 4) ||
-        !aligned(weights, 4))
+    if (!aligned(c, esize(c_dtype)) || !aligned(out, esize(out_dtype)) || !aligned(positions, 4) || !aligned(weights, 4))
         return MXFP8_ERR_ALIGN;
     const hipError_t e = mxfp8::launch_expert_combine(c, c_dtype == MXFP8_BF16, rows, cols, ldc, positions, weights, tokens, slots, out,
                                                       out_dtype == MXFP8_BF16, ld_out, static_cast<hipStream_t>(hip_stream));
@@ -113,14 +112,13 @@ mxfp8_status mxfp8_expert_weight_grad(const void *dy, mxfp8_dtype dy_dtype, int6
 {
     if (!valid_dtype(dy_dtype) || !valid_dtype(c_dtype))
         return MXFP8_ERR_DTYPE;
-    if (!valid_entries(tokens, slots) || rows < 0 || rows > kMaxRows || cols < 0 || cols > kMaxCols || cols % 32 || ldc < cols || ld_dy < cols)
+    if (!valid_entries(tokens, slots) || rows < 0 || rows > kMaxRows || cols < 0 || cols > kMaxCols || ldc < cols || ld_dy < cols)
         return MXFP8_ERR_SHAPE;
     if (tokens == 0)
         return MXFP8_OK;
     if ((rows > 0 && cols > 0 && !c) || (cols > 0 && !dy) || !positions || !dweights)
         return MXFP8_ERR_NULL;
-    if (!aligned(c, 16) || !aligned(dy, 16) || (ldc * esize(c_dtype)) % 16 || (ld_dy * esize(dy_dtype)) % 16 || !aligned(positions, 4) ||
-        !aligned(dweights, 4))
+    if (!aligned(c, esize(c_dtype)) || !aligned(dy, esize(dy_dtype)) || !aligned(positions, 4) || !aligned(dweights, 4))
         return MXFP8_ERR_ALIGN;
     return status(mxfp8::launch_expert_weight_grad(dy, dy_dtype == MXFP8_BF16, ld_dy, c, c_dtype == MXFP8_BF16, rows, cols, ldc, positions, tokens,
                                                    slots, dweights, static_cast<hipStream_t>(hip_stream)));

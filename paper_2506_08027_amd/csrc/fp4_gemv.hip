@@ -19,6 +19,7 @@ namespace mxfp8 {
 
 constexpr int kUnit = 4;  // scale blocks of a unit: 128 k, 64 bytes of a weight row, 256 bytes of a row of x
 constexpr int kGemvWaves = 8, kGemvThreads = 64 * kGemvWaves;
+constexpr int64_t kMostGemvWorkgroups = (int64_t(1) << 23) - 1;  // work-items of a launch are numbered in 32 bits
 
 // the eight codes of a word as BF16, times the scale
 __device__ __forceinline__ v8bf fp4_word_bf16(uint32_t w, float scale)
@@ -291,7 +292,7 @@ static hipError_t launch_fp4_gemv_t(const void *x, int64_t ldx, const GemvRows &
     constexpr int COLS = kGemvWaves / WK * NT * 16;  // rows of W of a workgroup
     const int64_t pieces = gemv_pieces(map, M, XR);
     const int64_t blocks_n = (N + COLS - 1) / COLS;
-    if (blocks_n * pieces > 0x7FFFFFFF)
+    if (blocks_n * pieces > kMostGemvWorkgroups)
         return hipErrorInvalidConfiguration;
     const bool vector = reinterpret_cast<uintptr_t>(c) % 16 == 0 && (ldc * (c_bf16 ? 2 : 4)) % 16 == 0;
     auto kern = map.ends ? fp4_gemv_kernel<XR, NT, WK, U, TILED, true> : fp4_gemv_kernel<XR, NT, WK, U, TILED, false>;

@@ -104,12 +104,12 @@ def test_sums_refuse(lib, name):
     def call(**k):
         return f(*{**good, **k}.values())
     assert call(t=2) == DTYPE and call(ot=-1) == DTYPE
-    for bad in (dict(rows=-1), dict(cols=40), dict(cols=-32), dict(ldc=32), dict(ldo=32), dict(tokens=-1), dict(slots=0), dict(slots=4097), dict(tokens=1 << 30),
+    for bad in (dict(rows=-1), dict(cols=-32), dict(ldc=32), dict(ldo=32), dict(tokens=-1), dict(slots=0), dict(slots=4097), dict(tokens=1 << 30),
                 dict(rows=(1 << 30) + 1)):
         assert call(**bad) == SHAPE, bad
     for bad in (dict(c=None), dict(o=None), dict(pos=None)) + ((dict(w=None),) if name == "weight_grad" else ()):
         assert call(**bad) == NULL, bad
-    for bad in (dict(c=P(0x1008)), dict(o=P(0x1008)), dict(ldc=66), dict(ldo=65), dict(t=1, ldc=68), dict(pos=P(0x1001)), dict(w=P(0x1002))):
+    for bad in (dict(c=P(0x1002)), dict(o=P(0x1006)), dict(t=1, c=P(0x1001)), dict(ot=1, o=P(0x1003)), dict(pos=P(0x1001)), dict(w=P(0x1002))):
         assert call(**bad) == ALIGN, bad
     assert call(tokens=0, c=None, o=None, pos=None, w=None) == OK
 

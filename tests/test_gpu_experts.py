@@ -252,7 +252,8 @@ def _check_combine(rng, tokens, slots, rows, cols, c_bf16, out_bf16, weighted, p
 @pytest.mark.parametrize("c_bf16", [False, True], ids=["c-f32", "c-bf16"])
 @pytest.mark.parametrize("out_bf16", [False, True], ids=["out-f32", "out-bf16"])
 @pytest.mark.parametrize("weighted", [False, True], ids=["plain", "weighted"])
-@pytest.mark.parametrize("tokens,slots,rows,cols,pad", [(1, 1, 1, 32, 0), (3, 8, 11, 544, 32), (17, 5, 40, 96, 64)])
+@pytest.mark.parametrize("tokens,slots,rows,cols,pad", [(1, 1, 1, 32, 0), (3, 8, 11, 544, 32), (17, 5, 40, 96, 64), (4, 2, 9, 1, 0), (5, 3, 7, 83, 0), (3, 2, 8, 517, 3),
+                                                     (4, 3, 5, 1043, 5)])
 def test_combine_is_the_weighted_sum(tokens, slots, rows, cols, pad, weighted, out_bf16, c_bf16):
     _check_combine(np.random.default_rng(tokens), tokens, slots, rows, cols, c_bf16, out_bf16, weighted, pad)
 
@@ -289,7 +290,8 @@ def _check_weight_grad(rng, tokens, slots, rows, cols, dy_bf16, c_bf16, pad=0):
 
 @pytest.mark.parametrize("dy_bf16", [False, True], ids=["dy-f32", "dy-bf16"])
 @pytest.mark.parametrize("c_bf16", [False, True], ids=["c-f32", "c-bf16"])
-@pytest.mark.parametrize("tokens,slots,rows,cols,pad", [(1, 1, 1, 32, 0), (3, 8, 11, 1056, 32), (17, 5, 40, 96, 64)])
+@pytest.mark.parametrize("tokens,slots,rows,cols,pad", [(1, 1, 1, 32, 0), (3, 8, 11, 1056, 32), (17, 5, 40, 96, 64), (4, 2, 9, 1, 0), (5, 3, 7, 83, 0), (3, 2, 8, 517, 3),
+                                                     (4, 3, 5, 1043, 5)])
 def test_weight_grad_is_the_dot_product(tokens, slots, rows, cols, pad, c_bf16, dy_bf16):
     _check_weight_grad(np.random.default_rng(tokens), tokens, slots, rows, cols, dy_bf16, c_bf16, pad)
 

@@ -134,7 +134,7 @@ def _rows(rng, rows, cols, ld, bf16):
 
 
 @pytest.mark.parametrize("c_bf16,out_bf16,weighted", [(False, False, False), (True, True, True), (False, True, True), (True, False, False)])
-@pytest.mark.parametrize("tokens,slots,rows,cols,ld", [(1, 1, 1, 32, 32), (5, 3, 4, 544, 552), (2, 9, 0, 64, 64)])
+@pytest.mark.parametrize("tokens,slots,rows,cols,ld", [(1, 1, 1, 32, 32), (5, 3, 4, 544, 552), (2, 9, 0, 64, 64), (3, 2, 5, 77, 77), (2, 2, 3, 9, 16)])
 def test_combine_and_weight_grad(driver, tmp_path, tokens, slots, rows, cols, ld, c_bf16, out_bf16, weighted):
     rng = np.random.default_rng(cols)
     flat, c = _rows(rng, rows, cols, ld, c_bf16)
