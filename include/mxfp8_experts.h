@@ -73,7 +73,7 @@ mxfp8_status mxfp8_expert_quantize_ex(const void *src, mxfp8_dtype src_dtype, in
  * sum, which is the gradient of the sorted copies), summed in FP32 in the order of j and rounded once. A position outside
  * [0, rows) adds nothing, whatever its weight; a token without any gets zeros. c [rows x cols] and out [tokens x cols] FP32 or
  * BF16, leading dimensions ldc, ld_out; positions [tokens x slots]; weights [tokens x slots] FP32 or NULL. Any cols; c and out aligned
- * to their element size (faster: they and their rows 16-byte aligned); positions and weights 4-byte aligned. Sizes as above, and
+ * to their element size (faster: cols % 8 == 0, they and their rows 16-byte aligned); positions and weights 4-byte aligned. Sizes as above, and
  * tokens * ceil(cols / 512) < 2^31.
  */
 mxfp8_status mxfp8_expert_combine(const void *c, mxfp8_dtype c_dtype, int64_t rows, int64_t cols, int64_t ldc,

@@ -161,22 +161,20 @@ hipError_t launch_expert_quantize(const void *src, bool bf16, int64_t tokens, in
 }
 
 // ---- sums over a token's rows --------------------------------------------------------------------------------------------------
-// Up to eight consecutive values as FP32, `n` of them there. VEC: 16-byte accesses where all eight are.
+// Up to eight consecutive values as FP32, `n` of them there. VEC: all eight always are, on 16 bytes.
 struct Values8 {
     float v[8];
 };
 template <bool BF16, bool VEC> __device__ __forceinline__ Values8 load8(const uint8_t *p, int n)
 {
     Values8 r = {};
-    if (!VEC || n < 8) {
+    if constexpr (!VEC) {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             if (k < n)
                 r.v[k] = BF16 ? __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(p)[k] << 16) : reinterpret_cast<const float *>(p)[k];
-        return r;
-    }
-    const uint4 a = *reinterpret_cast<const uint4 *>(p);
-    if constexpr (BF16) {
+    } else if constexpr (BF16) {
+        const uint4 a = *reinterpret_cast<const uint4 *>(p);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const uint32_t w = word_at(a, k);
@@ -184,7 +182,7 @@ template <bool BF16, bool VEC> __device__ __forceinline__ Values8 load8(const ui
             r.v[2 * k + 1] = __uint_as_float(w & 0xFFFF0000u);
         }
     } else {
-        const uint4 b = *reinterpret_cast<const uint4 *>(p + 16);
+        const uint4 a = *reinterpret_cast<const uint4 *>(p), b = *reinterpret_cast<const uint4 *>(p + 16);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             r.v[k] = __uint_as_float(word_at(a, k));
@@ -201,7 +199,7 @@ template <bool BF16, bool VEC> __device__ __forceinline__ void store8(uint8_t *p
         const v2bf h = {(__bf16)x.v[2 * k], (__bf16)x.v[2 * k + 1]};
         w[k] = __builtin_bit_cast(uint32_t, h);
     }
-    if (!VEC || n < 8) {
+    if constexpr (!VEC) {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             if (k < n) {
@@ -226,7 +224,8 @@ constexpr int kPiece = 512;  // columns of a wavefront: eight a lane
 constexpr int64_t kMostWorkgroups = int64_t(1) << 22;  // work-items of a launch are numbered in 32 bits: more work is walked over
 
 // A wavefront sums kPiece columns of one token; its rows and weights are the same for all lanes. What bounds it: HBM, the rows of c
-// once. BF16 [16384 tokens x 4 x 4096] 117 us = 5.7 TB/s; a few tokens take the launch.
+// once. BF16 [16384 tokens x 4 x 4096] 117 us = 5.7 TB/s; a few tokens take the launch ([3 x 8 x 2048] 3.2 us in a graph, where an empty
+// kernel takes 2.2; a row after the other 4.2).
 template <bool C_BF16, bool OUT_BF16, bool VEC>
 __global__ __launch_bounds__(kRowThreads) void expert_combine_kernel(const uint8_t *__restrict__ c, int64_t rows, int cols, int64_t ld_bytes,
                                                                      const int32_t *__restrict__ positions, const float *__restrict__ weights,
@@ -241,16 +240,24 @@ __global__ __launch_bounds__(kRowThreads) void expert_combine_kernel(const uint8
         if (n <= 0)
             continue;
         Values8 sum = {};
-        for (int j = 0; j < slots; ++j) {
-            const int64_t i = (int64_t)token * slots + j;
-            const int32_t r = positions[i];
-            if (r < 0 || r >= rows)
-                continue;
-            const float w = weights ? weights[i] : 1.0f;
-            const Values8 x = load8<C_BF16, VEC>(c + r * ld_bytes + col * (C_BF16 ? 2 : 4), n);
+        for (int j0 = 0; j0 < slots && rows > 0; j0 += 4) {  // four rows on their way at a time; those that are not there are read as row 0
+            const int64_t i = (int64_t)token * slots + j0;
+            Values8 x[4];
+            float w[4];
+            bool there[4];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                sum.v[k] = fmaf(w, x.v[k], sum.v[k]);
+            for (int j = 0; j < 4; ++j) {
+                const int32_t r = j0 + j < slots ? positions[i + j] : -1;
+                there[j] = r >= 0 && r < rows;
+                w[j] = weights && there[j] ? weights[i + j] : 1.0f;
+                x[j] = load8<C_BF16, VEC>(c + (there[j] ? r : 0) * ld_bytes + col * (C_BF16 ? 2 : 4), n);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (there[j])
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        sum.v[k] = fmaf(w[j], x[j].v[k], sum.v[k]);
         }
         store8<OUT_BF16, VEC>(out + token * ld_out_bytes + col * (OUT_BF16 ? 2 : 4), sum, n);
     }
@@ -267,7 +274,7 @@ hipError_t launch_expert_combine(const void *c, bool c_bf16, int64_t rows, int64
         return c_bf16 ? (out_bf16 ? expert_combine_kernel<true, true, V> : expert_combine_kernel<true, false, V>)
                       : (out_bf16 ? expert_combine_kernel<false, true, V> : expert_combine_kernel<false, false, V>);
     };
-    auto kern = on_16(c, ldc, c_bf16) && on_16(out, ld_out, out_bf16) ? pick(std::true_type{}) : pick(std::false_type{});
+    auto kern = cols % 8 == 0 && on_16(c, ldc, c_bf16) && on_16(out, ld_out, out_bf16) ? pick(std::true_type{}) : pick(std::false_type{});
     hipLaunchKernelGGL(kern, dim3((unsigned)workgroups), dim3(kRowThreads), 0, stream, static_cast<const uint8_t *>(c), rows, (int)cols,
                        ldc * (c_bf16 ? 2 : 4), positions, weights, (uint32_t)(tokens * pieces), slots, static_cast<uint8_t *>(out),
                        ld_out * (out_bf16 ? 2 : 4), (uint32_t)pieces);
@@ -276,7 +283,8 @@ hipError_t launch_expert_combine(const void *c, bool c_bf16, int64_t rows, int64
 
 // ---- gradient of the weights ------------------------------------------------------------------------------------------------------
 // A wavefront takes the dot product of one entry; the entries of a token lie side by side, so that its row of dy comes from the nearest
-// caches after the first of them. What bounds it: HBM. BF16 [8192 tokens x 2 x 5632] 46.7 us = 5.9 TB/s.
+// caches after the first of them. What bounds it: HBM. BF16 [8192 tokens x 2 x 5632] 49.2 us = 5.6 TB/s, [4096 x 8 x 2048] 29.8 (a piece
+// after the other 36.8), one token's 8 x 4096 3.2 (5.2).
 template <bool DY_BF16, bool C_BF16, bool VEC>
 __global__ __launch_bounds__(kRowThreads) void expert_weight_grad_kernel(const uint8_t *__restrict__ dy, int64_t ld_dy_bytes, const uint8_t *__restrict__ c,
                                                                          int64_t rows, int cols, int64_t ld_bytes,
@@ -286,17 +294,32 @@ __global__ __launch_bounds__(kRowThreads) void expert_weight_grad_kernel(const u
     const int lane = threadIdx.x & 63;
     for (uint32_t i = blockIdx.x * kRowWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); i < entries; i += gridDim.x * kRowWaves) {
         const int32_t r = positions[i];
-        float sum = 0.0f;
+        Values8 part = {};
         if (r >= 0 && r < rows) {
             const uint8_t *a = dy + (int64_t)(i / slots) * ld_dy_bytes, *b = c + r * ld_bytes;
-            for (int64_t col = lane * 8; col < cols; col += kPiece) {
+            int64_t col = lane * 8;
+            for (; col + 3 * kPiece + 8 <= cols; col += 4 * kPiece) {  // four pieces on their way at a time
+                Values8 x[4], y[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[j] = load8<DY_BF16, VEC>(a + (col + j * kPiece) * (DY_BF16 ? 2 : 4), 8);
+                    y[j] = load8<C_BF16, VEC>(b + (col + j * kPiece) * (C_BF16 ? 2 : 4), 8);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        part.v[k] = fmaf(x[j].v[k], y[j].v[k], part.v[k]);
+            }
+            for (; col < cols; col += kPiece) {
                 const int n = (int)min((int64_t)cols - col, (int64_t)8);
                 const Values8 x = load8<DY_BF16, VEC>(a + col * (DY_BF16 ? 2 : 4), n), y = load8<C_BF16, VEC>(b + col * (C_BF16 ? 2 : 4), n);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    sum = fmaf(x.v[k], y.v[k], sum);
+                    part.v[k] = fmaf(x.v[k], y.v[k], part.v[k]);
             }
         }
+        float sum = ((part.v[0] + part.v[1]) + (part.v[2] + part.v[3])) + ((part.v[4] + part.v[5]) + (part.v[6] + part.v[7]));
         for (int d = 32; d >= 1; d /= 2)
             sum += __uint_as_float((uint32_t)__shfl_xor((int)__float_as_uint(sum), d, 64));
         if (lane == 0)
@@ -313,7 +336,7 @@ hipError_t launch_expert_weight_grad(const void *dy, bool dy_bf16, int64_t ld_dy
         return dy_bf16 ? (c_bf16 ? expert_weight_grad_kernel<true, true, V> : expert_weight_grad_kernel<true, false, V>)
                        : (c_bf16 ? expert_weight_grad_kernel<false, true, V> : expert_weight_grad_kernel<false, false, V>);
     };
-    auto kern = on_16(c, ldc, c_bf16) && on_16(dy, ld_dy, dy_bf16) ? pick(std::true_type{}) : pick(std::false_type{});
+    auto kern = cols % 8 == 0 && on_16(c, ldc, c_bf16) && on_16(dy, ld_dy, dy_bf16) ? pick(std::true_type{}) : pick(std::false_type{});
     hipLaunchKernelGGL(kern, dim3((unsigned)workgroups), dim3(kRowThreads), 0, stream, static_cast<const uint8_t *>(dy), ld_dy * (dy_bf16 ? 2 : 4),
                        static_cast<const uint8_t *>(c), rows, (int)cols, ldc * (c_bf16 ? 2 : 4), positions, (uint32_t)entries, (uint32_t)slots, dw);
     return hipGetLastError();
