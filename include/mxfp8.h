@@ -18,7 +18,8 @@
  * tiled layout and a bound on the workgroups (_ex); the product that also emits the MXFP8 copies of its output;
  * E5M2 elements and the OCP v1 scale rule of the paper's ablations (_mode_ex, for quantize, dequantize and the
  * product); the BF16 product of the simulated path; grouped products for mixture-of-experts layers; the column
- * copy derived from a kept row copy; the MXFP4 and MXFP6 members of Table 1; and measurement aids.
+ * copy derived from a kept row copy; the MXFP4 and MXFP6 members of Table 1; and measurement aids. What surrounds the grouped
+ * products of a mixture-of-experts layer, and products of a few rows with MXFP4 weights, are declared in mxfp8_experts.h.
  *
  * Conventions common to every entry point
  *   - All data pointers are DEVICE pointers (HIP global memory of the current device). The

@@ -94,10 +94,10 @@ mxfp8_status mxfp8_expert_weight_grad(const void *dy, mxfp8_dtype dy_dtype, int6
  * C [M x N] = x [M x K] * W [N x K]^T for a few rows of BF16 activations and MXFP4 weights as mxfp8_fp4_quantize_ex stores them
  * (w_q [N x K/2], w_s [N x K/32] in `scale_layout`): the weights are widened to BF16, as mxfp8_fp4_dequantize_ex gives them, on their
  * way to the matrix instructions and accumulated in FP32; activations are not quantized. c FP32 or BF16 (RNE), leading dimension
- * ldc >= N. Meant for up to some tens of rows, where reading the weights is all the work; any M is right. M, N <= 2^30, K <= 2^24, at most 2^23 - 1 workgroups (of 16
- * rows of W and 32 of x or more, each expert's rows apart; else MXFP8_ERR_SHAPE),
- * K % 32 == 0 (K == 0 stores zeros); x 16-byte aligned and ldx a multiple of 8; w_q and tiled w_s 16-byte aligned; c aligned to its
- * element size (faster: c and its rows 16-byte aligned). A 0xFF scale makes its output column NaN.
+ * ldc >= N. Meant for up to some thirty rows, where reading the weights is all the work; any M is right. M, N <= 2^30, K <= 2^24,
+ * ceil(N / 16) * M < 2^23 (products of many rows are taken up to 32 times that, then MXFP8_ERR_SHAPE); K % 32 == 0 (K == 0 stores
+ * zeros); x 16-byte aligned and ldx a multiple of 8; w_q and tiled w_s 16-byte aligned; c aligned to its element size (faster: c and
+ * its rows 16-byte aligned). A 0xFF scale makes its output column NaN.
  */
 mxfp8_status mxfp8_fp4_gemv_ex(const void *x_bf16, int64_t ldx, const uint8_t *w_q, const uint8_t *w_s, int64_t M, int64_t N,
                                int64_t K, void *c, mxfp8_dtype c_dtype, int64_t ldc, mxfp8_scale_layout scale_layout,
