@@ -12,7 +12,7 @@
 //   result is dropped: a load under a condition would have to be waited for before the loads behind it.
 //   Measured in a captured graph, where an empty kernel takes 2.2 us: [1 x 4096 x 4096] 4.8 us, [1 x 4096 x 14336] 10.2 and [1 x 28672 x 4096]
 //   15.5 (31 and 62 MB of weights; what comes on top of the first takes HBM's time, 5 to 5.5 TB/s), 48 tokens x 4 of 64 experts [5632 x 2048]
-//   73 (5.3 TB/s). With more rows the copies of x that each workgroup fetches from L2 take over: [12 x 4096 x 14336] 14.4 us (88 MB of x
+//   73 (5.3 TB/s). With more rows the copies of x that each workgroup fetches from L2 take over: [12 x 4096 x 14336] 14.1 us (88 MB of x
 //   beside 31 of W), [64 x 28672 x 4096] 44.
 #include "expert_launches.h"
 #include "gemm_device.h"
@@ -98,6 +98,38 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
     if (p.count <= 0)
         return;
 
+    // ---- rows of W: four lanes a row, from block 4u + lane % 4 on; scales of the next four units, one dword a lane
+    const int n0 = ((int)block * WN + wn) * NT * 16;
+    const int s_unit = TILED ? g : lane & 3, s_row = TILED ? r : lane >> 2;
+    const uint8_t *wq[NT], *ws[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int w_row = min(n0 + t * 16 + (lane >> 2), N - 1), s_n = min(n0 + t * 16 + s_row, N - 1);
+        wq[t] = w_q + p.expert * (GROUPED ? map.wq_group_bytes : 0) + w_row * ((int64_t)nb * 16) + (lane & 3) * 16;
+        ws[t] = w_s + p.expert * (GROUPED ? map.ws_group_bytes : 0) + (TILED ? ((int64_t)(s_n >> 6) * ((nb + 3) / 4) * 64 + (s_n & 63)) * 4 : (int64_t)s_n * nb);
+    }
+
+    struct Units {
+        uint4 w[NT][U], x[XL];
+        uint32_t s[NT];
+    };
+    const int whole = nb / kUnit, begin = (int)((int64_t)whole * wk / WK), end = (int)((int64_t)whole * (wk + 1) / WK);
+    auto load_w = [&](Units &d, int u) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int j = 0; j < U; ++j)
+                d.w[t][j] = stream_load(reinterpret_cast<const uint4 *>(wq[t] + (int64_t)min(u + j, end - 1) * 64));
+            __builtin_memcpy(&d.s[t], ws[t] + (int64_t)min(u + s_unit, end - 1) * (TILED ? 256 : 4), 4);
+        }
+        MXFP8_PIN();
+    };
+    // The first weights are requested before the rows of x are worked out: 6.2 -> 5.5 us for 16 rows of a 4096 x 4096 matrix. With
+    // experts the entries of the plan go first, or their rows of x wait behind the weights: 6.4 us, against 6.9, for 8 experts' 2048 x 1408.
+    Units d;
+    if (!GROUPED && begin < end)
+        load_w(d, begin);
+
     // ---- rows of x of the columns that this lane has of C (-1: zeros), and of the pieces that it loads
     int at[MT];
     uint64_t any = 0;
@@ -122,34 +154,10 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
         const int row = U == 4 ? __builtin_amdgcn_readlane(at[m / 16], m % 16) : __shfl(at[m / 16], (m + lane_row) % 16, 64);
         xp[q] = x + (row < 0 ? first_row : row) * ldx_bytes + lane_piece * 16;
     }
-    // ---- rows of W: four lanes a row, from block 4u + lane % 4 on; scales of the next four units, one dword a lane
-    const int n0 = ((int)block * WN + wn) * NT * 16;
-    const int s_unit = TILED ? g : lane & 3, s_row = TILED ? r : lane >> 2;
-    const uint8_t *wq[NT], *ws[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int w_row = min(n0 + t * 16 + (lane >> 2), N - 1), s_n = min(n0 + t * 16 + s_row, N - 1);
-        wq[t] = w_q + p.expert * (GROUPED ? map.wq_group_bytes : 0) + w_row * ((int64_t)nb * 16) + (lane & 3) * 16;
-        ws[t] = w_s + p.expert * (GROUPED ? map.ws_group_bytes : 0) + (TILED ? ((int64_t)(s_n >> 6) * ((nb + 3) / 4) * 64 + (s_n & 63)) * 4 : (int64_t)s_n * nb);
-    }
-
-    struct Units {
-        uint4 w[NT][U], x[XL];
-        uint32_t s[NT];
-    };
     uint4 *const lds_x = staged[wave], *const lds_w = lds_x + XP;
     uint32_t *const lds_s = reinterpret_cast<uint32_t *>(lds_w + WP);
     v4f acc[NT][MT] = {};
-    const int units = any ? nb / kUnit : 0;  // whole ones
-    const int begin = (int)((int64_t)units * wk / WK), end = (int)((int64_t)units * (wk + 1) / WK);
-    auto load = [&](Units &d, int u) __attribute__((always_inline)) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int j = 0; j < U; ++j)
-                d.w[t][j] = stream_load(reinterpret_cast<const uint4 *>(wq[t] + (int64_t)min(u + j, end - 1) * 64));
-            __builtin_memcpy(&d.s[t], ws[t] + (int64_t)min(u + s_unit, end - 1) * (TILED ? 256 : 4), 4);
-        }
+    auto load_x = [&](Units &d, int u) __attribute__((always_inline)) {
         const int last = (end - u) * 16 - 1;  // pieces of x behind the last unit are not multiplied: any others will do
 #pragma unroll
         for (int q = 0; q < XL; ++q)
@@ -209,31 +217,34 @@ __global__ __launch_bounds__(kGemvThreads) void fp4_gemv_kernel(const uint8_t *_
         MXFP8_PIN();
     };
     // The next units are on their way while those in LDS are multiplied.
-    if (begin < end) {
-        Units d;
-        load(d, begin);
+    if (any && begin < end) {
+        if (GROUPED)
+            load_w(d, begin);
+        load_x(d, begin);
         for (int u = begin; u < end; u += U) {
             stage(d);
-            if (u + U < end)
-                load(d, u + U);
+            if (u + U < end) {
+                load_w(d, u + U);
+                load_x(d, u + U);
+            }
             multiply(end - u);
         }
     }
     if (any && nb % kUnit && wk == WK - 1) {  // one to three blocks behind the whole units
         const int rest = nb % kUnit;
-        Units d = {};
+        d = {};
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             if ((lane & 3) < rest)
-                d.w[t][0] = *reinterpret_cast<const uint4 *>(wq[t] + (int64_t)units * 64);
+                d.w[t][0] = *reinterpret_cast<const uint4 *>(wq[t] + (int64_t)whole * 64);
             if (s_unit == 0)
                 for (int b = 0; b < rest; ++b)
-                    d.s[t] |= (uint32_t)ws[t][(int64_t)units * (TILED ? 256 : 4) + b] << (8 * b);
+                    d.s[t] |= (uint32_t)ws[t][(int64_t)whole * (TILED ? 256 : 4) + b] << (8 * b);
         }
         if (lane_piece < rest * 4)
 #pragma unroll
             for (int q = 0; q < XL; ++q)
-                d.x[q] = *reinterpret_cast<const uint4 *>(xp[q] + (int64_t)units * 256);
+                d.x[q] = *reinterpret_cast<const uint4 *>(xp[q] + (int64_t)whole * 256);
         stage(d);
         multiply(1);
     }
