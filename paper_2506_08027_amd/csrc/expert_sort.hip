@@ -73,7 +73,7 @@ __global__ __launch_bounds__(kSortThreads) void expert_sort_kernel(const ID *__r
         own[i] = 0;
     __syncthreads();
     if (counts == nullptr) {
-        for (int i = tid; i < entries; i += n) {
+        for (int i = tid; groups > 0 && i < entries; i += n) {  // more than kOneLaunch entries only come here without experts
             const int e = expert_of(experts, i, groups);
             if (e < groups) {
                 atomicAdd(total + e, 1u);

@@ -97,6 +97,22 @@ def test_sort_full_size(entries, groups, align, index64):
     _check_sort(_experts(np.random.default_rng(entries), entries, 1, groups), groups, align, 11, index64)
 
 
+def test_sort_of_many_entries_without_experts_full_size():
+    """Each entry is looked at once, as with an expert, not once by each of the 8192 workgroups (tens of milliseconds)."""
+    experts = torch.zeros((1 << 23, 1), dtype=torch.int32, device="cuda")
+    took = []
+    for groups in (1, 0, 1, 0):
+        plan = mx.expert_sort(experts, groups, 1)
+        start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        mx.expert_sort(experts, groups, 1)
+        end.record()
+        torch.cuda.synchronize()
+        took.append(start.elapsed_time(end))
+    assert (plan["positions"] == -1).all() and (plan["sources"] == -1).all()
+    assert took[3] < 8 * took[2], took
+
+
 # ---- quantizer of sorted rows -------------------------------------------------------------------------------------------------
 
 def _check_quantize(src, src32, experts, groups, align, slots, weights, axis, tiled, extra_rows=0, rows=None, whole=False):
