@@ -2,7 +2,7 @@
  * mxfp8_experts.h -- C ABI of what surrounds the products of a mixture-of-experts layer (Appendix A.4: the recipe applies unchanged
  * to the expert products), and of products of a few rows with MXFP4 weights. Same library and conventions as mxfp8.h: device
  * pointers, the caller owns every buffer, nothing is allocated, kept or synchronised, work goes to `hip_stream`, errors by
- * return code before any launch.
+ * return code before any launch. No output overlaps an input or another output.
  *
  *   training  mxfp8_expert_sort(experts, align = 128)                       plan
  *             mxfp8_expert_quantize_ex(x, no weights, MXFP8_BOTH)           X_row, X_colT of the sorted rows

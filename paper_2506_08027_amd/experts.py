@@ -24,6 +24,13 @@ def _ready(*tensors):
         raise ValueError(f"the tensors live on {device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
+def _int32(value, what):
+    """A number that ctypes would cut down to 32 bits without a word."""
+    if not -2 ** 31 <= value < 2 ** 31:
+        raise ValueError(f"{what} is {value}")
+    return value
+
+
 def _check_index(t, numel, what):
     if t.dtype != torch.int32 or not t.is_contiguous() or (numel is not None and t.numel() != numel):
         raise ValueError(f"{what} must be contiguous int32" + ("" if numel is None else f" of {numel} elements"))
@@ -55,7 +62,7 @@ def _fast(name, what, *args) -> bool:
 
 def mxfp8_expert_rows(entries: int, groups: int, align: int) -> int:
     """Rows that sorted entries take at most (host arithmetic in the library)."""
-    n = _b.load().mxfp8_expert_rows(entries, groups, align)
+    n = _b.load().mxfp8_expert_rows(entries, _int32(groups, "groups"), _int32(align, "align"))
     if n < 0:
         raise ValueError("bad number of entries, groups or alignment")
     return n
@@ -63,7 +70,7 @@ def mxfp8_expert_rows(entries: int, groups: int, align: int) -> int:
 
 def mxfp8_expert_sort_workspace(entries: int, groups: int) -> int:
     """Bytes of workspace that mxfp8_expert_sort needs (host arithmetic in the library)."""
-    n = _b.load().mxfp8_expert_sort_workspace(entries, groups)
+    n = _b.load().mxfp8_expert_sort_workspace(entries, _int32(groups, "groups"))
     if n < 0:
         raise ValueError("bad number of entries or groups")
     return n
@@ -77,7 +84,7 @@ def mxfp8_expert_sort(experts, align, positions, sources, group_ends, workspace=
     _ready(experts, positions, sources, group_ends, workspace)
     if experts.dtype not in (torch.int32, torch.int64) or not experts.is_contiguous():
         raise ValueError("experts must be contiguous int32 or int64")
-    entries, groups = experts.numel(), group_ends.numel()
+    entries, groups, align = experts.numel(), group_ends.numel(), _int32(align, "align")
     _check_index(positions, entries, "positions")
     _check_index(sources, None, "sources")
     _check_index(group_ends, None, "group_ends")
@@ -99,7 +106,7 @@ def mxfp8_expert_quantize_ex(src, sources, group_ends, slots, weights, axis, q_r
     ld = _matrix(src, "src")
     tokens, cols = src.shape
     _check_index(sources, None, "sources")
-    rows = sources.numel()
+    rows, slots = sources.numel(), _int32(slots, "slots")
     if group_ends is not None:
         _check_index(group_ends, None, "group_ends")
         if not group_ends.numel():
@@ -188,7 +195,7 @@ def mxfp8_fp4_gemv_grouped_ex(x, sources, slots, w_q, w_s, group_ends, c, scale_
         raise ValueError("c must be [rows x N]")
     M, N = c.shape
     _check_index(group_ends, None, "group_ends")
-    groups = group_ends.numel()
+    groups, slots = group_ends.numel(), _int32(slots, "slots")
     if sources is not None:
         _check_index(sources, M, "sources")
     elif tokens < M:
@@ -218,7 +225,8 @@ def expert_sort(experts, groups, align=128):
 
 
 def expert_quantize(src, sources, group_ends, slots, weights=None, axis="both", scale_layout=SCALES_ROWMAJOR):
-    """Allocate outputs and call mxfp8_expert_quantize_ex; keys as for quantize()."""
+    """Allocate outputs and call mxfp8_expert_quantize_ex; keys as for quantize(). Rows behind the last 128-row tile that holds a row of
+    an expert are not written: they hold whatever the allocation held."""
     rows, cols = sources.numel(), src.shape[1]
     ax = _b._AXIS[axis]
     out = {}

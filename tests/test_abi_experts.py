@@ -165,6 +165,12 @@ def test_binding_names_what_is_wrong():
         (ValueError, "int32 or int64", lambda: mx.mxfp8_expert_sort(i32(4, 4)[:, :2], 1, i32(8), i32(8), i32(4))),
         (ValueError, "positions must be", lambda: mx.mxfp8_expert_sort(i32(4, 2), 1, i32(7), i32(8), i32(4))),
         (ValueError, "workspace", lambda: mx.mxfp8_expert_sort(i32(1 << 20), 1, i32(1 << 20), i32(1 << 20), i32(4))),
+        (ValueError, "align is", lambda: mx.mxfp8_expert_sort(i32(4, 2), 2 ** 32 + 1, i32(8), i32(8), i32(4))),
+        (ValueError, "align is", lambda: mx.mxfp8_expert_rows(8, 4, 2 ** 32 + 1)),
+        (ValueError, "groups is", lambda: mx.mxfp8_expert_rows(8, 2 ** 32 + 4, 1)),
+        (ValueError, "groups is", lambda: mx.mxfp8_expert_sort_workspace(8, 4 - 2 ** 32)),
+        (ValueError, "slots is", lambda: mx.mxfp8_expert_quantize_ex(f32(4, 64), i32(64), i32(2), 2 ** 32 + 2, None, "rowwise", u8(64, 64), u8(64, 2))),
+        (ValueError, "slots is", lambda: mx.mxfp8_fp4_gemv_grouped_ex(bf(2, 64), i32(4), 2 ** 32 + 2, u8(3, 4, 32), u8(3, 4, 2), i32(3), f32(4, 4))),
         (mx.MXFP8Error, "bad shape", lambda: mx.mxfp8_expert_sort(i32(4, 2), 4, i32(8), i32(8), i32(4))),
         (ValueError, "multiples of 32", lambda: mx.mxfp8_expert_quantize_ex(f32(4, 64), i32(40), i32(2), 2, None, "rowwise", u8(40, 64), u8(40, 2))),
         (ValueError, "q_row", lambda: mx.mxfp8_expert_quantize_ex(f32(4, 64), i32(64), i32(2), 2, None, "rowwise", u8(32, 64), u8(64, 2))),
