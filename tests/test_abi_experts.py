@@ -203,3 +203,16 @@ def test_binding_names_what_is_wrong():
     finally:
         binding._need_cuda, binding._stream = keep
     assert experts.MXFP8Error is mx.MXFP8Error
+
+
+def test_calls_in_cpp_leave_other_arguments_to_python():
+    """-1: not handled; the binding then names what is wrong."""
+    from paper_2506_08027_amd import binding
+    binding.load()
+    if binding._fast is None:
+        pytest.skip("the module of the calls in C++ is not built")
+    host = torch.zeros((4, 64), dtype=torch.bfloat16)
+    for name, n in (("expert_sort", 7), ("expert_quantize", 12), ("expert_combine", 5), ("expert_weight_grad", 5), ("fp4_gemv", 6), ("fp4_gemv_grouped", 9)):
+        call = getattr(binding._fast, name)
+        for args in ((), (host,) * n, (None,) * n, ("x",) * n, (host,) * (n + 1)):
+            assert call(*args) == -1, (name, len(args))
