@@ -14,15 +14,10 @@
 #define __launch_bounds__(...)
 #define __shared__ static  // one workgroup runs at a time, so a static array is that workgroup's LDS
 
-struct alignas(8) uint2 {
-    uint32_t x, y;
-};
-struct alignas(16) uint4 {
-    uint32_t x, y, z, w;
-};
-struct alignas(16) float4 {
-    float x, y, z, w;
-};
+// (vectors, not structures: a copy of a structure is not checked for its alignment)
+typedef uint32_t uint2 __attribute__((ext_vector_type(2)));
+typedef uint32_t uint4 __attribute__((ext_vector_type(4)));
+typedef float float4 __attribute__((ext_vector_type(4)));
 inline uint2 make_uint2(uint32_t x, uint32_t y) { return uint2{x, y}; }
 inline uint4 make_uint4(uint32_t x, uint32_t y, uint32_t z, uint32_t w) { return uint4{x, y, z, w}; }
 inline float4 make_float4(float x, float y, float z, float w) { return float4{x, y, z, w}; }
