@@ -52,9 +52,10 @@ template <bool SRC_BF16, bool WEIGHTED> struct ExpertRows {
             }
         }
         if constexpr (WEIGHTED) {
-            // Ties and borders of the conversion end in 19 zero bits: only where a product does (one tile of a wavefront in a hundred, with
-            // weights that are not powers of two) does it matter how it was rounded. (The same tensor: never asking 29.3 us, always rounding to
-            // odd 40.8, this way 33.0.)
+            // Ties and borders of the conversion end in 19 zero bits: only where a product does can it matter how it was rounded, in dense data
+            // with weights that are not powers of two one tile of a wavefront in a hundred. Zeros, and BF16 values times powers of two, end in
+            // them too although their products are exact. (The same tensor: never asking 29.3 us, always rounding to odd 40.8, this way 32.7;
+            // with 0.1 | 1 | 10 % of the tokens zero 34.7 | 38.5 | 41.3, with weights of 1 41.4. FP32 37.4, with 1 % of the tokens zero 43.1.)
             uint32_t low = ~0u;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -114,12 +115,12 @@ __global__ __launch_bounds__(kQuantThreads) void expert_quantize_kernel(
             const uint32_t i = r < rows ? (uint32_t)sources[r] : ~0u;
             token[tid] = i < entries ? (int32_t)(i / slots) : -1;
             if constexpr (WEIGHTED)
-                weight[tid] = i < entries ? weights[i] : 1.1f;  // of rows that become zeros: no border
+                weight[tid] = i < entries ? weights[i] : 1.1f;  // of rows that become zeros: as good as never a border but for zeros of row 0
         }
         __syncthreads();
         quantize_tile<BF16, ROW, COL, TILED, 0, false>(nullptr, rows, cols, 0, q_row, s_row, q_colT, s_colT, nullptr, tile_y, tile_x, tid, lds,
                                                        &rows_of_tile);
-        __syncthreads();  // the next tile reuses the arrays
+        __syncthreads();  // between two tiles, as quantize_tile wants it (the barriers behind the next rows and within the tile would do)
     }
 }
 
@@ -224,7 +225,7 @@ constexpr int kPiece = 512;  // columns of a wavefront: eight a lane
 constexpr int64_t kMostWorkgroups = int64_t(1) << 22;  // work-items of a launch are numbered in 32 bits: more work is walked over
 
 // A wavefront sums kPiece columns of one token; its rows and weights are the same for all lanes. What bounds it: HBM, the rows of c
-// once. BF16 [16384 tokens x 4 x 4096] 117 us = 5.7 TB/s; a few tokens take the launch ([3 x 8 x 2048] 3.2 us in a graph, where an empty
+// once. BF16 [16384 tokens x 4 x 4096] 117 us = 5.8 TB/s; a few tokens take the launch ([3 x 8 x 2048] 3.2 us in a graph, where an empty
 // kernel takes 2.2; a row after the other 4.2).
 template <bool C_BF16, bool OUT_BF16, bool VEC>
 __global__ __launch_bounds__(kRowThreads) void expert_combine_kernel(const uint8_t *__restrict__ c, int64_t rows, int cols, int64_t ld_bytes,
@@ -282,9 +283,10 @@ hipError_t launch_expert_combine(const void *c, bool c_bf16, int64_t rows, int64
 }
 
 // ---- gradient of the weights ------------------------------------------------------------------------------------------------------
-// A wavefront takes the dot product of one entry; the entries of a token lie side by side, so that its row of dy comes from the nearest
-// caches after the first of them. What bounds it: HBM. BF16 [8192 tokens x 2 x 5632] 49.2 us = 5.6 TB/s, [4096 x 8 x 2048] 29.8 (a piece
-// after the other 36.8), one token's 8 x 4096 3.2 (5.2).
+// A wavefront takes the dot product of one entry, a workgroup those of four entries side by side. The row of dy of a token with more slots, or
+// with slots that four does not divide, is fetched by several workgroups, which lie on different XCDs with an L2 each: [1003 tokens x 6 x 2880]
+// fetches dy, 11.6 MB, 1.9 times. What bounds it: HBM. BF16 [8192 x 2 x 5632] 46.9 us = 5.9 TB/s launched one after the other and 49.2 in
+// a captured graph, [4096 x 8 x 2048] 29.4 there (a piece after the other 36.8), one token's 8 x 4096 3.2 (5.2).
 template <bool DY_BF16, bool C_BF16, bool VEC>
 __global__ __launch_bounds__(kRowThreads) void expert_weight_grad_kernel(const uint8_t *__restrict__ dy, int64_t ld_dy_bytes, const uint8_t *__restrict__ c,
                                                                          int64_t rows, int cols, int64_t ld_bytes,

@@ -10,10 +10,11 @@
 //   14336] 17.4 us). So four neighbouring lanes load 64 bytes of a row of W and 16 lanes 256 bytes of a row of x, and each
 //   wavefront reorders them through an LDS area of its own. Rows that are not there are read from one that is, and their column of the
 //   result is dropped: a load under a condition would have to be waited for before the loads behind it.
-//   Measured in a captured graph, where an empty kernel takes 2.2 us: [1 x 4096 x 4096] 4.8 us, [1 x 4096 x 14336] 10.2 and [1 x 28672 x 4096]
-//   15.5 (31 and 62 MB of weights; what comes on top of the first takes HBM's time, 5 to 5.5 TB/s), 48 tokens x 4 of 64 experts [5632 x 2048]
-//   73 (5.3 TB/s). With more rows the copies of x that each workgroup fetches from L2 take over: [12 x 4096 x 14336] 14.1 us (88 MB of x
-//   beside 31 of W), [64 x 28672 x 4096] 44.
+//   Measured in a captured graph, where an empty kernel takes 2.2 us: [1 x 4096 x 4096] 5.0 us, [1 x 4096 x 14336] 10.4 and [1 x 28672 x 4096]
+//   15.6 (9, 31 and 62 MB of weights: what comes on top of the first goes at 4.1 TB/s where K is long, at 5.0 where there are many rows
+//   of W), 48 tokens x 4 of 64 experts [5632 x 2048] 74 (45 to 53 of the experts are chosen, 280 to 330 MB: 4.2 TB/s). With more rows
+//   the copies of x that each workgroup fetches from L2 take over: [12 x 4096 x 14336] 14.2 us (88 MB of x beside 31 of W),
+//   [64 x 28672 x 4096] 44.
 #include "expert_launches.h"
 #include "gemm_device.h"
 
