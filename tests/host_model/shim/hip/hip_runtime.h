@@ -56,8 +56,6 @@ inline uint32_t atomicAdd(uint32_t *p, uint32_t v)  // one fiber runs at a time
 
 #define __builtin_amdgcn_readfirstlane(x) ::wavesim::readfirstlane(x)
 #define __builtin_amdgcn_readlane(x, l) ::wavesim::shfl((int)(x), (l))
-#define __builtin_amdgcn_permlane32_swap(a, b, fi, bc) ::wavesim::permlane_swap((a), (b), 32)
-#define __builtin_amdgcn_permlane16_swap(a, b, fi, bc) ::wavesim::permlane_swap((a), (b), 16)
 #define __builtin_amdgcn_s_waitcnt(imm) ::wavesim::s_waitcnt(imm)
 #define __builtin_amdgcn_sched_barrier(mask) ((void)0)
 #define __builtin_amdgcn_s_barrier() ::wavesim::block_sync()

@@ -257,23 +257,6 @@ inline int shfl(int v, int src)
 }
 inline int shfl_xor(int v, int mask) { return shfl(v, g.cur->lane ^ mask); }
 
-// v_permlane{32,16}_swap_b32: the upper half of the lanes (the odd rows of 16) of the first register changes places with the lower half (the
-// even rows) of the second
-typedef unsigned int v2ui __attribute__((ext_vector_type(2)));
-inline v2ui permlane_swap(uint32_t a, uint32_t b, int distance)
-{
-    struct Pub {
-        uint32_t a, b;
-    } pub{a, b};
-    Wave &w = publish(pub);
-    const int lane = g.cur->lane, other = lane ^ distance;
-    if (!w.present[other])
-        fail("a lane swap reads lane %d, which is not active", other);
-    const Pub o = peek<Pub>(w, other);
-    unpublish();
-    return lane & distance ? v2ui{o.b, b} : v2ui{a, o.a};
-}
-
 inline uint64_t ballot(bool b)
 {
     Wave &w = publish((int)b);
