@@ -123,15 +123,14 @@ def build(work, text, name="gemm.hip"):
     csrc = os.path.join(work, "csrc")
     shutil.copytree(os.path.join(ROOT, "paper_2506_08027_amd", "csrc"), csrc)
     open(os.path.join(csrc, name), "w").write(text)
-    inc = os.path.join(ROOT, "include", "mxfp8.h")
-    for name, path in (("api.hip", csrc), ("driver.cpp", work)):
-        src = os.path.join(csrc if name == "api.hip" else HERE, name)
-        text = open(src).read().replace('"../../include/mxfp8.h"', f'"{inc}"').replace('"wavesim.h"', f'"{HERE}/wavesim.h"')
-        open(os.path.join(path, name), "w").write(text)
+    shutil.copy(os.path.join(HERE, "driver.cpp"), work)
+    sources = [os.path.join(csrc, f) for f in sorted(os.listdir(csrc)) if f.endswith(".hip")]
+    for path in sources + [os.path.join(work, "driver.cpp")]:   # the copies lie elsewhere than the headers
+        text = open(path).read()
+        open(path, "w").write(text.replace('"../../include/', f'"{ROOT}/include/').replace('"wavesim.h"', f'"{HERE}/wavesim.h"'))
     binary = os.path.join(work, "hostmodel")
     cmd = ["/opt/rocm/llvm/bin/clang++", "-std=c++17", "-x", "c++", "-I", os.path.join(HERE, "shim"), "-O0",
-           "-Wno-unknown-pragmas", "-Wno-psabi", "-o", binary, os.path.join(work, "driver.cpp")]
-    cmd += [os.path.join(csrc, f) for f in sorted(os.listdir(csrc)) if f.endswith(".hip")]
+           "-Wno-unknown-pragmas", "-Wno-psabi", "-o", binary, os.path.join(work, "driver.cpp"), *sources]
     subprocess.run(cmd, check=True, capture_output=True)
     return binary
 
