@@ -171,7 +171,8 @@ __global__ __launch_bounds__(Cfg::THREADS, 2) void b128_gemm_kernel(const uint8_
             const int i = row_of(m), j = col_of(m);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                acc[i][j][e] = __builtin_fmaf(VECTORS ? p[m % P][e] * cols[VECTORS ? j : 0][e] : p[m % P][e], scale[i % SETS], acc[i][j][e]);
+                // the scales' product first: the sum times one of them alone can leave FP32, and this waits for no matrix instruction
+                acc[i][j][e] = __builtin_fmaf(p[m % P][e], VECTORS ? cols[VECTORS ? j : 0][e] * scale[i % SETS] : scale[i % SETS], acc[i][j][e]);
             // with that, column j is done with its fragment and scales
             if (NEXT && i == TM - 1)
                 read_b(kt + 1, j);
