@@ -51,15 +51,17 @@ int64_t mxfp8_b128_gemm_workspace(mxfp8_pass pass, int64_t M, int64_t N, int64_t
 
 /*
  * C [M x N] = A [M x K] * B [N x K]^T: C[m, n] = sum over blocks b of a_s * b_s * sum over k in b of A[m, k] B[n, k], each block's sum
- * on the matrix instructions (which cut every product of eight neighbours off at 2^-13 of the largest of them), scaled and added up in FP32. A is cut into VECTORS; B into TILES in MXFP8_FPROP and MXFP8_DGRAD,
- * into VECTORS in MXFP8_WGRAD (the operand table above). The product of two scales is formed in FP32: one beyond its range
- * counts as infinite, one below 2^-126 as a subnormal.
+ * on the matrix instructions, scaled and added up in FP32. The type of c chooses how a block's sum is made: for BF16 by the FP8 instructions,
+ * which cut every product of eight neighbours off at 2^-13 of the largest of them (below the result's rounding); for FP32 from the
+ * codes widened to BF16, exactly, with FP32 additions, at half the rate. A is cut into VECTORS; B into TILES in MXFP8_FPROP and
+ * MXFP8_DGRAD, into VECTORS in MXFP8_WGRAD (the operand table above). The product of two scales is formed in FP32, before the block's sum is
+ * multiplied with it: one beyond its range counts as infinite, one below 2^-126 as a subnormal.
  * c FP32 or BF16 (rounded to nearest even), leading dimension ldc >= N, aligned to its element size (faster: c and its rows
  * 16-byte aligned). Any M, N up to 2^30 and K up to 2^24, ceil(M / 32) * ceil(N / 32) < 2^31 (otherwise MXFP8_ERR_SHAPE); K == 0 stores
  * zeros. a_q, b_q 16-byte aligned, lda, ldb multiples of 16 below 2^24 + 16; scales 4-byte aligned.
  * workspace: mxfp8_b128_gemm_workspace bytes, 16-byte aligned, contents meaningless before and after (the sums of parts of K, where
  * there are few tiles); calls that may run at the same time, captured graphs among them, need one each.
- * A NaN in an element or a scale makes every output that it touches NaN. The order of the sums depends on the sizes alone.
+ * A NaN in an element or a scale makes every output that it touches NaN. The order of the sums depends on the sizes and the type of c alone.
  */
 mxfp8_status mxfp8_b128_gemm(mxfp8_pass pass, const uint8_t *a_q, int64_t lda, const float *a_s, const uint8_t *b_q, int64_t ldb,
                              const float *b_s, int64_t M, int64_t N, int64_t K, void *c, mxfp8_dtype c_dtype, int64_t ldc,
