@@ -510,9 +510,9 @@ PyObject *expert_layer(PyObject *, PyObject *const *args, Py_ssize_t n)
     const Values v = values(*x, tokens, hidden), o = values(*out, tokens, hidden);
     const bool wide = experts->scalar_type() == at::kLong;
     if (!v.ok || v.dtype != 1 || !o.ok || tokens > kMany || slots < 1 || slots > 4096 || groups < 1 || groups > 4096 || inter > kMany || hidden > kMany ||
-        (!wide && experts->scalar_type() != at::kInt) || !experts->is_contiguous() || experts->size(0) != tokens || !weights_ok(weights, tokens * slots) ||
-        !expert_matrices(*up_q, *up_s, format, groups, 2 * inter, hidden, layout) ||
-        !expert_matrices(*down_q, *down_s, format, groups, hidden, inter, layout) ||
+        (!wide && experts->scalar_type() != at::kInt) || !experts->is_contiguous() || experts->size(0) != tokens ||
+        weights->sizes() != experts->sizes() || !weights_ok(weights, tokens * slots) ||
+        !expert_matrices(*up_q, *up_s, format, groups, 2 * inter, hidden, layout) || !expert_matrices(*down_q, *down_s, format, groups, hidden, inter, layout) ||
         !holds(workspace, reinterpret_cast<int64_t (*)(I, int32_t, I)>(entry[EXPERT_LAYER_WORKSPACE])(tokens, (int32_t)slots, inter)) ||
         !on_current_device({x, experts, weights, up_q, up_s, down_q, down_s, out, workspace}))
         return not_handled();

@@ -47,8 +47,8 @@ def mxfp8_expert_layer(x, experts, weights, format, up_q, up_s, down_q, down_s, 
     if experts.dtype not in (torch.int32, torch.int64) or not experts.is_contiguous() or experts.dim() != 2 or experts.shape[0] != tokens:
         raise ValueError(f"experts must be contiguous int32 or int64 [{tokens} x slots]")
     slots = experts.shape[1]
-    if weights is None:
-        raise ValueError("the layer needs the router's weights")
+    if weights is None or tuple(weights.shape) != (tokens, slots):
+        raise ValueError(f"the layer needs the router's weights, contiguous float32 [{tokens} x {slots}]")
     _check_weights(weights, tokens * slots)
     if down_q.dim() != 3:
         raise ValueError("down_q must be [groups x hidden x inter]")
