@@ -74,8 +74,9 @@ def mxfp8_b128_gemm_workspace(pass_, M: int, N: int, K: int) -> int:
 
 
 def mxfp8_b128_gemm(pass_, a_q, a_s, b_q, b_s, c, workspace=None, stream=None) -> None:
-    """c [M x N] (float32/bfloat16) = A [M x K] B [N x K]^T; A in vectors, B in tiles ("wgrad": in vectors). workspace: uint8 of
-    mxfp8_b128_gemm_workspace(pass_, M, N, K) bytes, None where that is 0."""
+    """c [M x N] (float32/bfloat16) = A [M x K] B [N x K]^T; A in vectors, B in tiles ("wgrad": in vectors). A float32 c is made of exact
+    products at half the rate, a bfloat16 one by the FP8 instructions. workspace: uint8 of mxfp8_b128_gemm_workspace(pass_, M, N, K) bytes,
+    None where that is 0."""
     if _fast("b128_gemm", "mxfp8_b128_gemm", pass_, a_q, a_s, b_q, b_s, c, workspace, stream):
         return
     _ready(a_q, a_s, b_q, b_s, c, workspace)

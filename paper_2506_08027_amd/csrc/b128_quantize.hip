@@ -10,7 +10,7 @@
 // 2^-60 (but not 0), where one could be, and blocks with infinities or NaN take the division instead, in code of its own.
 //   What bounds it: HBM, with one read and two write streams. BF16 [8192 x 4096], both copies 28 us (4.8 TB/s), row copy 19.8 (5.1); FP32
 // [14336 x 4096] in tiles, both copies 66.7 (5.3); FP32 [1999 x 5632], both copies 19.2: there the values take 64 registers and their
-// conversion 168 in all, two workgroups of four wavefronts to a unit, and 704 tiles one and a half rounds.
+// conversion 168 in all, three workgroups of four wavefronts to a unit: 704 tiles are one round, whose reads, conversions and writes overlap little.
 #include "b128_launches.h"
 #include "mxfp8_device.h"
 

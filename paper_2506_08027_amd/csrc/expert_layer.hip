@@ -1,4 +1,4 @@
-// A whole mixture-of-experts layer for a few tokens (include/mxfp8_experts.h) in two kernels: the up-projections with the gate, and the
+// A whole mixture-of-experts layer for a few tokens (include/mxfp8_layer.h) in two kernels: the up-projections with the gate, and the
 // down-projections with the sum over a token's experts. The stream of a wavefront is described in few_rows.h.
 //
 // First kernel. A workgroup has some tiles of 16 of an expert's `inter` values, gate and other rows of W side by side, for all
@@ -13,7 +13,7 @@
 // Tokens are taken 64 at a time (a chunk), each with its own workgroups.
 // Where 16 columns a workgroup leave units idle, several share them and the one that arrives last adds up their sums.
 // Measured in a captured graph, weights from HBM: 48 tokens x 4 of 64 experts, [2048 x 2816], scales for 128 x 128: 173 us, 6.1 TB/s, what
-// a large read reaches; 4 x 8 [2048 x 1408], MXFP8: 51 (4.6). 1 x 8, MXFP4: 19 us for 37 MB. Of these 6.6 are two launches with nothing
+// a large read reaches (180 on another card); 4 x 8 [2048 x 1408], MXFP8: 51 (4.6). 1 x 8, MXFP4: 19 us for 37 MB. Of these 6.6 are two launches with nothing
 // to read but the plan, 2 finding rows and joining sums; the up-projections' 25 MB arrive at 5.3 TB/s, the down-projections' 12 take 4 us,
 // h and the plan having come from other units first.
 #include "expert_launches.h"
