@@ -1,5 +1,5 @@
-"""FP32 results of the products with a scale for each block of 128 on the CPU execution model: the GPU tests of their accuracy replayed, and BF16
-results of the larger tiles, which FP32 results do not take, with AddressSanitizer."""
+"""Both kinds of results of the products with a scale for each block of 128 on the CPU execution model: the GPU tests of FP32 results' accuracy and of
+BF16 results replayed, and BF16 results of the larger tiles, which FP32 results do not take, with AddressSanitizer."""
 import numpy as np
 import pytest
 
@@ -10,8 +10,8 @@ from test_host_model_experts import ORDERS, Case, driver  # noqa: F401
 from test_host_model_replay_b128 import hostmodel_lib, test_gpu_tests_pass_on_the_host_model as _replay  # noqa: F401
 
 
-@pytest.mark.parametrize("file,at_least", [("test_gpu_b128_fp32.py", 42)])
-def test_gpu_tests_of_fp32_results_pass_on_the_host_model(hostmodel_lib, file, at_least):  # noqa: F811
+@pytest.mark.parametrize("file,at_least", [("test_gpu_b128_fp32.py", 42), ("test_gpu_b128_bf16.py", 20)])
+def test_gpu_tests_of_both_results_pass_on_the_host_model(hostmodel_lib, file, at_least):  # noqa: F811
     _replay(hostmodel_lib, file, at_least)
 
 
